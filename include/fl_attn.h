@@ -334,6 +334,96 @@ fl_status fl_attn_prefill_paged(const fl_tensor* q, const fl_tensor* k_cache, co
  * (each rounded up to 256). */
 size_t fl_attn_prefill_paged_workspace_size(const fl_tensor* q, const fl_tensor* k_cache, const fl_paged_kv* kv);
 
+/* ---- a bounded key/value cache: positions turned into queries and keys, the weight that cached keys receive, eviction by it ---- */
+
+/* Rotary positions with several axes (time, height, width): channel pair i of a query or key turns by the angle
+ * t = positions[b, s, axis of i] * inv_freq[i],
+ *     (x_a, x_b)  ->  (x_a cos t - x_b sin t,  x_b cos t + x_a sin t).
+ * The pairs follow the axes in order, sections[0] pairs the first axis, then sections[1] the second, ...; with `pairs` of them in all,
+ * pair i is the channels (i, i + pairs), or (2i, 2i + 1) when interleaved, and channels from 2 * pairs on stay as they are. */
+typedef struct {
+  uint32_t       struct_size;   /* sizeof(fl_rotary) */
+  uint32_t       axes;          /* 1 .. 4                                                                     */
+  int32_t        sections[4];   /* pairs per axis, >= 0; 1 <= their sum, twice that <= D                      */
+  uint32_t       interleaved;   /* 0 | 1                                                                      */
+  uint32_t       inverse;       /* 1: turns by -t (the gradient of the call with 0, and its inverse)          */
+  const int32_t* positions;     /* device [B, S, axes] of any value                                           */
+  int64_t        stride[3];     /* its element strides (0 broadcasts, e.g. over the batch)                    */
+  const float*   inv_freq;      /* device [pairs], contiguous                                                 */
+} fl_rotary;
+
+/* Turns q and k (either may be NULL, with its output).  The angle is reduced in 64 bits, so positions of any size keep
+ * their phase; products are in 32 bits and rounded once.
+ *   q  [B, 1, H, S, D],  k  [B, 1, Hkv, S, D]   bf16 or f32, one dtype; any D
+ *   q_out, k_out   of the same sizes and dtype; may be q and k themselves (in place), no other overlap
+ * Stream, ownership and error rules as for fl_attn_fwd; empty tensors return FL_OK without a launch. */
+fl_status fl_rotary_embed(const fl_tensor* q, const fl_tensor* k, const fl_rotary* rotary, fl_tensor* q_out, fl_tensor* k_out, void* stream);
+
+/* The serving form: q, k and v of each sequence's T newest tokens (T = 1: the token being generated; more: a prompt chunk).
+ * Writes the turned queries to q_out, and the turned keys and the values to the tokens' slots of the paged cache, len_b - T .. len_b - 1
+ * (kv->seq_lens counts the new tokens already, as in the fl_attn_decode or fl_attn_prefill_paged call that follows).  Positions are the
+ * caller's: a slot need not say where its token is in the sequence, so that a cache some tokens have been evicted from goes on as it is.
+ *   q [B, 1, H, T, D], k and v [B, 1, Hkv, T, D]  bf16;  q_out as q (may be q itself);  rotary->inverse 0
+ *   k_cache, v_cache, kv   as for fl_attn_decode, any D; written here.  Nothing is written for tokens at negative slots (len_b < T)
+ *                          and for those whose table entry names no page of the cache. */
+fl_status fl_rotary_append(const fl_tensor* q, const fl_tensor* k, const fl_tensor* v, const fl_rotary* rotary, const fl_paged_kv* kv,
+                           fl_tensor* q_out, fl_tensor* k_cache, fl_tensor* v_cache, void* stream);
+
+/* fl_attn_decode that also adds up what weight each cached key receives: with P the probabilities of the call's rows,
+ *     weights[b, hkv, j]  =  (j < len_b - T ? weights[b, hkv, j] : 0)  +  sum of P over the T rows and the query heads of hkv
+ * for j < len_b: the T newest tokens start at zero, so the array needs no clearing when a sequence starts or grows.
+ *   weights   [B, 1, Hkv, 1, C] f32, C >= kv->max_seq_len, unit inner stride: one row per sequence and kv head, in slot order
+ *             (not in pages: sequences that share pages keep their own weights); slots from len_b on are left alone
+ *   aux       workspace of fl_attn_decode_weights_workspace_size bytes
+ * Everything else, and out and lse, as for fl_attn_decode.  Results are bitwise reproducible (no atomics). */
+fl_status fl_attn_decode_weights(const fl_tensor* q, const fl_tensor* k_cache, const fl_tensor* v_cache,
+                                 const fl_paged_kv* kv, const fl_variant_desc* desc, const fl_aux* aux,
+                                 fl_tensor* out, fl_tensor* lse, fl_tensor* weights, void* stream);
+
+/* Bytes of aux->workspace that fl_attn_decode_weights needs: fl_attn_decode's and the scores, 4 bytes each, which wait there until the
+ * last split has been seen. */
+size_t fl_attn_decode_weights_workspace_size(const fl_tensor* q, const fl_tensor* k_cache, const fl_paged_kv* kv);
+
+/* The same update of `weights` from a chunk of Sq prompt rows, whose log-sum-exp fl_attn_prefill_paged has written:
+ * P = exp(s - lse) is formed again tile by tile and summed over rows and query heads, never stored.
+ *   q         [B, 1, H, Sq, D] bf16, D in {32, 64, 128}: the newest Sq tokens of every sequence, as in the fl_attn_prefill_paged call
+ *   k_cache, kv, desc, aux->alibi_slopes   as in that call (rows at negative positions and keys that a row does not see add nothing)
+ *   lse       [B, 1, H, Sq, 1] f32
+ *   weights   [B, 1, Hkv, 1, C] f32, as for fl_attn_decode_weights with T = Sq
+ *   aux       workspace of fl_key_weights_workspace_size bytes (may be 0, then aux may be NULL without alibi_slopes)
+ * Results are bitwise reproducible (no atomics). */
+fl_status fl_key_weights(const fl_tensor* q, const fl_tensor* k_cache, const fl_tensor* lse, const fl_paged_kv* kv,
+                         const fl_variant_desc* desc, const fl_aux* aux, fl_tensor* weights, void* stream);
+
+/* Bytes of aux->workspace that fl_key_weights needs: partial sums, where few sequences are cut over many workgroups. */
+size_t fl_key_weights_workspace_size(const fl_tensor* q, const fl_tensor* k_cache, const fl_paged_kv* kv);
+
+/* What eviction keeps, and where it puts it. */
+typedef struct {
+  uint32_t       struct_size;   /* sizeof(fl_evict) */
+  int32_t        budget;        /* tokens kept of a longer sequence, >= 1                                        */
+  int32_t        sinks;         /* the first and the newest slots of a sequence stay whatever their weight:      */
+  int32_t        recent;        /* sinks + recent <= budget                                                      */
+  const int32_t* dst_table;     /* device [B, dst_stride]: pages of the same caches that take what stays, at least
+                                   budget / page_size of them (rounded up) per sequence; none of them is a page that
+                                   any sequence of the call is read from (not checked)                           */
+  int32_t        dst_stride;
+  int32_t        reserved;
+  int32_t*       new_lens;      /* device [B], written: min(len_b, budget)                                       */
+  int32_t*       kept;          /* device [B, Hkv, budget], written: the slots that stay, ascending, then -1     */
+} fl_evict;
+
+/* Eviction from a paged cache by accumulated weight.  Of every sequence and kv head min(len_b, budget) tokens stay: the first `sinks`, the
+ * newest `recent`, and of the others those of the largest weight (of equal weights those in lower slots; a NaN is less than every number).
+ * Their keys and values are copied, in slot order, to slots 0 .. of the pages in dst_table; the pages they came from are left as they are,
+ * the caller's to hand out again.  Different kv heads keep different tokens: a slot of the result is no longer one position.
+ *   weights       [B, 1, Hkv, 1, C] f32, C >= kv->max_seq_len, as the calls above have left them
+ *   k_cache, v_cache, kv   as for fl_attn_decode (any D, bf16); with a page size that is a power of two >= 8, also without a block table
+ *   new_weights   [B, 1, Hkv, 1, C2] f32, C2 >= budget, unit inner stride; not `weights`: the weights of what stays, zero from new_lens[b] to C2
+ * Nothing is copied to a destination whose table entry names no page of the cache. */
+fl_status fl_cache_evict(const fl_tensor* weights, fl_tensor* k_cache, fl_tensor* v_cache, const fl_paged_kv* kv, const fl_evict* evict,
+                         fl_tensor* new_weights, void* stream);
+
 /* A variant compiled at run time from user expressions (opaque; owned by the caller until released). */
 typedef struct fl_custom_variant fl_custom_variant;
 

@@ -54,6 +54,16 @@ class fl_paged_kv(C.Structure):
                 ("max_seq_len", C.c_int32), ("reserved2", C.c_int32)]
 
 
+class fl_rotary(C.Structure):
+    _fields_ = [("struct_size", C.c_uint32), ("axes", C.c_uint32), ("sections", C.c_int32 * 4), ("interleaved", C.c_uint32),
+                ("inverse", C.c_uint32), ("positions", C.c_void_p), ("stride", C.c_int64 * 3), ("inv_freq", C.c_void_p)]
+
+
+class fl_evict(C.Structure):
+    _fields_ = [("struct_size", C.c_uint32), ("budget", C.c_int32), ("sinks", C.c_int32), ("recent", C.c_int32), ("dst_table", C.c_void_p),
+                ("dst_stride", C.c_int32), ("reserved", C.c_int32), ("new_lens", C.c_void_p), ("kept", C.c_void_p)]
+
+
 class FlError(RuntimeError):
     def __init__(self, status: int, text: str, detail: str):
         super().__init__(f"fl_attn status {status} ({text}): {detail}")
@@ -105,6 +115,21 @@ def lib() -> C.CDLL:
         L.fl_attn_prefill_paged.argtypes = L.fl_attn_decode.argtypes
         L.fl_attn_prefill_paged_workspace_size.restype = C.c_size_t
         L.fl_attn_prefill_paged_workspace_size.argtypes = [TP, TP, C.POINTER(fl_paged_kv)]
+        L.fl_rotary_embed.restype = C.c_int
+        L.fl_rotary_embed.argtypes = [TP, TP, C.POINTER(fl_rotary), TP, TP, C.c_void_p]
+        L.fl_rotary_append.restype = C.c_int
+        L.fl_rotary_append.argtypes = [TP, TP, TP, C.POINTER(fl_rotary), C.POINTER(fl_paged_kv), TP, TP, TP, C.c_void_p]
+        L.fl_attn_decode_weights.restype = C.c_int
+        L.fl_attn_decode_weights.argtypes = [TP, TP, TP, C.POINTER(fl_paged_kv), C.POINTER(fl_variant_desc), C.POINTER(fl_aux), TP, TP, TP,
+                                             C.c_void_p]
+        L.fl_attn_decode_weights_workspace_size.restype = C.c_size_t
+        L.fl_attn_decode_weights_workspace_size.argtypes = [TP, TP, C.POINTER(fl_paged_kv)]
+        L.fl_key_weights.restype = C.c_int
+        L.fl_key_weights.argtypes = [TP, TP, TP, C.POINTER(fl_paged_kv), C.POINTER(fl_variant_desc), C.POINTER(fl_aux), TP, C.c_void_p]
+        L.fl_key_weights_workspace_size.restype = C.c_size_t
+        L.fl_key_weights_workspace_size.argtypes = [TP, TP, C.POINTER(fl_paged_kv)]
+        L.fl_cache_evict.restype = C.c_int
+        L.fl_cache_evict.argtypes = [TP, TP, TP, C.POINTER(fl_paged_kv), C.POINTER(fl_evict), TP, C.c_void_p]
         L.fl_compile_variant.restype = C.c_int
         L.fl_compile_variant.argtypes = [C.c_char_p, C.c_char_p, C.c_uint32, C.c_int, C.POINTER(C.c_void_p)]
         L.fl_attn_fwd_custom.restype = C.c_int
@@ -146,7 +171,8 @@ def lib() -> C.CDLL:
 
 EXPORTS = ["fl_attn_fwd", "fl_attn_fwd_noalloc", "fl_attn_fwd_workspace_size", "fl_attn_bwd", "fl_attn_bwd_workspace_size", "fl_attn_bwd_ex", "fl_attn_bwd_ex_workspace_size",
            "fl_bwd_supported", "fl_attn_decode", "fl_attn_decode_workspace_size", "fl_attn_prefill_paged", "fl_attn_prefill_paged_workspace_size", "fl_compile_variant", "fl_attn_fwd_custom", "fl_compile_variant_aux", "fl_attn_fwd_custom_aux", "fl_attn_fwd_custom_skip", "fl_custom_skip_workspace_size", "fl_compile_variant_grad", "fl_attn_bwd_custom", "fl_attn_bwd_custom_workspace_size",
-           "fl_release_variant", "fl_variant_supported", "fl_strerror",
+           "fl_rotary_embed", "fl_rotary_append", "fl_attn_decode_weights", "fl_attn_decode_weights_workspace_size", "fl_key_weights",
+           "fl_key_weights_workspace_size", "fl_cache_evict", "fl_release_variant", "fl_variant_supported", "fl_strerror",
            "fl_last_error_detail", "fl_set_tuning", "fl_version"]
 
 
@@ -291,6 +317,73 @@ def fl_attn_prefill_paged(q: fl_tensor, k_cache: fl_tensor, v_cache: fl_tensor, 
 
 def fl_attn_prefill_paged_workspace_size(q: fl_tensor, k_cache: fl_tensor, kv: fl_paged_kv) -> int:
     return lib().fl_attn_prefill_paged_workspace_size(_ref(q), _ref(k_cache), _ref(kv))
+
+
+def rotary_desc(positions, inv_freq, sections: Sequence[int], *, interleaved: bool = False, inverse: bool = False) -> fl_rotary:
+    """positions: int32 device tensor [B, S, axes]; inv_freq: float32 [sum(sections)]."""
+    r = fl_rotary()
+    r.struct_size = C.sizeof(fl_rotary)
+    r.axes, r.interleaved, r.inverse = len(sections), int(interleaved), int(inverse)
+    for a, n in enumerate(sections[:4]):
+        r.sections[a] = n
+    r.positions, r.inv_freq = positions.data_ptr(), inv_freq.data_ptr()
+    for a in range(3):
+        r.stride[a] = positions.stride(a)
+    return r
+
+
+def weights_desc(t) -> fl_tensor:
+    """fl_tensor of accumulated weights [B, Hkv, C]."""
+    return tensor_desc(t[:, None, :, None])
+
+
+def evict_desc(*, budget: int, sinks: int, recent: int, dst_table, new_lens, kept) -> fl_evict:
+    e = fl_evict()
+    e.struct_size = C.sizeof(fl_evict)
+    e.budget, e.sinks, e.recent = budget, sinks, recent
+    e.dst_table, e.dst_stride = dst_table.data_ptr(), dst_table.stride(0)
+    e.new_lens, e.kept = new_lens.data_ptr(), kept.data_ptr()
+    return e
+
+
+def fl_rotary_embed(q: Optional[fl_tensor], k: Optional[fl_tensor], rotary: fl_rotary, q_out: Optional[fl_tensor], k_out: Optional[fl_tensor],
+                    stream: int = 0) -> int:
+    """Raw call; returns the fl_status code."""
+    return lib().fl_rotary_embed(_ref(q), _ref(k), _ref(rotary), _ref(q_out), _ref(k_out), C.c_void_p(stream))
+
+
+def fl_rotary_append(q: fl_tensor, k: fl_tensor, v: fl_tensor, rotary: fl_rotary, kv: fl_paged_kv, q_out: fl_tensor, k_cache: fl_tensor,
+                     v_cache: fl_tensor, stream: int = 0) -> int:
+    """Raw call; returns the fl_status code."""
+    return lib().fl_rotary_append(_ref(q), _ref(k), _ref(v), _ref(rotary), _ref(kv), _ref(q_out), _ref(k_cache), _ref(v_cache),
+                                  C.c_void_p(stream))
+
+
+def fl_attn_decode_weights(q: fl_tensor, k_cache: fl_tensor, v_cache: fl_tensor, kv: fl_paged_kv, desc: fl_variant_desc, aux: Optional[fl_aux],
+                           out: fl_tensor, lse: Optional[fl_tensor], weights: fl_tensor, stream: int = 0) -> int:
+    """Raw call; returns the fl_status code."""
+    return lib().fl_attn_decode_weights(_ref(q), _ref(k_cache), _ref(v_cache), _ref(kv), _ref(desc), _ref(aux), _ref(out), _ref(lse),
+                                        _ref(weights), C.c_void_p(stream))
+
+
+def fl_attn_decode_weights_workspace_size(q: fl_tensor, k_cache: fl_tensor, kv: fl_paged_kv) -> int:
+    return lib().fl_attn_decode_weights_workspace_size(_ref(q), _ref(k_cache), _ref(kv))
+
+
+def fl_key_weights(q: fl_tensor, k_cache: fl_tensor, lse: fl_tensor, kv: fl_paged_kv, desc: fl_variant_desc, aux: Optional[fl_aux],
+                   weights: fl_tensor, stream: int = 0) -> int:
+    """Raw call; returns the fl_status code."""
+    return lib().fl_key_weights(_ref(q), _ref(k_cache), _ref(lse), _ref(kv), _ref(desc), _ref(aux), _ref(weights), C.c_void_p(stream))
+
+
+def fl_key_weights_workspace_size(q: fl_tensor, k_cache: fl_tensor, kv: fl_paged_kv) -> int:
+    return lib().fl_key_weights_workspace_size(_ref(q), _ref(k_cache), _ref(kv))
+
+
+def fl_cache_evict(weights: fl_tensor, k_cache: fl_tensor, v_cache: fl_tensor, kv: fl_paged_kv, evict: fl_evict, new_weights: fl_tensor,
+                   stream: int = 0) -> int:
+    """Raw call; returns the fl_status code."""
+    return lib().fl_cache_evict(_ref(weights), _ref(k_cache), _ref(v_cache), _ref(kv), _ref(evict), _ref(new_weights), C.c_void_p(stream))
 
 
 def fl_compile_variant(score_mod: Optional[str], mask: Optional[str], D: int, base_mask: int = 0):

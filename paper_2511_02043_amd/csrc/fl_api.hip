@@ -31,7 +31,10 @@ static __device__ __align__(256) unsigned char scratch[kScratchBytes];
 
 namespace {
 
+using fl::host::canonical_mask;
 using fl::host::check_data_tensor;
+using fl::host::check_desc;
+using fl::host::clamp_window;
 using fl::host::fail;
 using fl::host::g_detail;
 using fl::host::make_view;
@@ -64,40 +67,6 @@ struct Registry {
 const Registry& registry() {
   static Registry r;
   return r;
-}
-
-// A window that reaches past both sequence ends changes nothing; cutting it there keeps the kernels'
-// int32 arithmetic on i - window and j + window far from overflow (callers pass INT_MAX for "no limit").
-int32_t clamp_window(int32_t window, int64_t Sq, int64_t Sk) {
-  const int64_t lim = Sq > Sk ? Sq : Sk;
-  return (int64_t)window > lim ? (int32_t)lim : window;
-}
-
-// Canonical mask bits: WINDOW implies CAUSAL.
-uint32_t canonical_mask(uint32_t m) { return (m & FL_MASK_WINDOW) ? (m | FL_MASK_CAUSAL) : m; }
-
-fl_status check_desc(const fl_variant_desc* d) {
-  if (d == nullptr) return fail(FL_ERR_NULL, "desc is NULL");
-  if (d->struct_size != sizeof(fl_variant_desc))
-    return fail(FL_ERR_DESC, "desc->struct_size = %u, expected %zu", d->struct_size, sizeof(fl_variant_desc));
-  if (!(d->scale > 0.f) || !std::isfinite(d->scale)) return fail(FL_ERR_DESC, "scale must be finite and > 0");
-  if (d->score_mod > FL_MOD_SOFTCAP) return fail(FL_ERR_DESC, "unknown score_mod %u", d->score_mod);
-  if (d->score_mod == FL_MOD_SOFTCAP && (!(d->softcap > 0.f) || !std::isfinite(d->softcap)))
-    return fail(FL_ERR_DESC, "softcap must be finite and > 0");
-  if (d->mask & ~(uint32_t)(FL_MASK_CAUSAL | FL_MASK_WINDOW | FL_MASK_DOC | FL_MASK_PREFIX))
-    return fail(FL_ERR_DESC, "unknown mask bits 0x%x", d->mask);
-  if ((d->mask & FL_MASK_PREFIX) && (d->mask & (FL_MASK_CAUSAL | FL_MASK_WINDOW)))
-    return fail(FL_ERR_DESC, "FL_MASK_PREFIX excludes FL_MASK_CAUSAL and FL_MASK_WINDOW");
-  if ((d->mask & FL_MASK_WINDOW) && d->window < 0) return fail(FL_ERR_DESC, "window must be >= 0");
-  if ((d->mask & FL_MASK_PREFIX) && d->prefix_len < 0) return fail(FL_ERR_DESC, "prefix_len must be >= 0");
-  if (d->n_bias > 2) return fail(FL_ERR_DESC, "n_bias must be 0..2");
-  if (d->combine > FL_DIFFERENTIAL) return fail(FL_ERR_DESC, "unknown combine %u", d->combine);
-  if (d->epilogue & ~(uint32_t)(FL_EPI_RMSNORM | FL_EPI_GATE_SIGMOID))
-    return fail(FL_ERR_DESC, "unknown epilogue bits 0x%x", d->epilogue);
-  if ((d->epilogue & FL_EPI_RMSNORM) && (!(d->rms_eps >= 0.f) || !std::isfinite(d->rms_eps)))
-    return fail(FL_ERR_DESC, "rms_eps must be finite and >= 0");
-  if (d->q_offset < 0 || d->q_offset > 0x3fffffff) return fail(FL_ERR_DESC, "q_offset must be in [0, 2^30)");
-  return FL_OK;
 }
 
 // Sk > 0: the key length of the call, for the shape preference; <= 0: any shape of the variant will do.
@@ -485,9 +454,9 @@ BwdWorkspace bwd_workspace(int64_t B, int64_t G, int64_t H, int64_t Hkv, int64_t
   return w;
 }
 
-const fl::DecodeEntry* find_decode_entry(int D, int mod, int cb, int waves) {
+const fl::DecodeEntry* find_decode_entry(int D, int mod, int cb, int waves, bool weights) {
   int n = 0;
-  const fl::DecodeEntry* tab = fl::entries_decode(&n);
+  const fl::DecodeEntry* tab = weights ? fl::entries_decode_weights(&n) : fl::entries_decode(&n);
   for (int i = 0; i < n; ++i)
     if (tab[i].D == D && tab[i].mod == mod && tab[i].cb == cb && tab[i].waves == waves) return &tab[i];
   return nullptr;
@@ -2282,8 +2251,25 @@ size_t fl_attn_decode_workspace_size(const fl_tensor* q, const fl_tensor* k_cach
   return (size_t)(B * T * H * ns) * (size_t)(D + 2) * sizeof(float);
 }
 
-fl_status fl_attn_decode(const fl_tensor* q, const fl_tensor* k_cache, const fl_tensor* v_cache, const fl_paged_kv* kv,
-                         const fl_variant_desc* desc, const fl_aux* aux, fl_tensor* out, fl_tensor* lse, void* stream_v) {
+// Bytes of the scores that fl_attn_decode_weights keeps in the workspace, behind the partial results.
+static size_t decode_score_bytes(int64_t B, int64_t T, int64_t H, int64_t max_seq_len) {
+  return max_seq_len > 0 ? (size_t)(B * T * H) * (size_t)((max_seq_len + 31) / 32) * 32 * sizeof(float) : 0;
+}
+// The partial results, rounded up so that the scores start 16-byte aligned.
+static size_t decode_partial_bytes(int64_t B, int64_t T, int64_t H, int64_t D, int ns) {
+  return ((size_t)(B * T * H * ns) * (size_t)(D + 2) * sizeof(float) + 255) / 256 * 256;
+}
+
+size_t fl_attn_decode_weights_workspace_size(const fl_tensor* q, const fl_tensor* k_cache, const fl_paged_kv* kv) {
+  if (q == nullptr || k_cache == nullptr || kv == nullptr) return 0;
+  const int64_t B = q->size[0], H = q->size[2], T = q->size[3], D = q->size[4];
+  const int ns = decode_splits(B, k_cache->size[2], D, kv->max_seq_len);
+  return decode_partial_bytes(B, T, H, D, ns) + decode_score_bytes(B, T, H, kv->max_seq_len);
+}
+
+// `weights`: null for fl_attn_decode
+static fl_status decode_call(const fl_tensor* q, const fl_tensor* k_cache, const fl_tensor* v_cache, const fl_paged_kv* kv,
+                             const fl_variant_desc* desc, const fl_aux* aux, fl_tensor* out, fl_tensor* lse, fl_tensor* weights, void* stream_v) {
   g_detail[0] = 0;
   fl_status st = check_desc(desc);
   if (st != FL_OK) return st;
@@ -2325,7 +2311,8 @@ fl_status fl_attn_decode(const fl_tensor* q, const fl_tensor* k_cache, const fl_
   const int ns = decode_splits(B, Hkv, D, kv->max_seq_len), cb = H > 0 && (H / Hkv) * T > 32 ? 2 : 1;
   // a window's keys, from the oldest query row's first one, begin anywhere in a tile
   const int64_t reach = (mask & FL_MASK_WINDOW) != 0 && desc->window >= 0 ? std::min<int64_t>(kv->max_seq_len, desc->window + T + 31) : kv->max_seq_len;
-  const fl::DecodeEntry* de = find_decode_entry((int)D, (int)desc->score_mod, cb, decode_waves(D, cb, B * Hkv * ns, (reach + 32 * ns - 1) / (32 * ns)));
+  const fl::DecodeEntry* de = find_decode_entry((int)D, (int)desc->score_mod, cb, decode_waves(D, cb, B * Hkv * ns, (reach + 32 * ns - 1) / (32 * ns)),
+                                                weights != nullptr);
   if (de == nullptr || v_cache->size[4] != D)
     return fail(FL_ERR_UNSUPPORTED, "no decode specialisation for D=%lld Dv=%lld score_mod=%u", (long long)D,
                 (long long)v_cache->size[4], desc->score_mod);
@@ -2349,14 +2336,17 @@ fl_status fl_attn_decode(const fl_tensor* q, const fl_tensor* k_cache, const fl_
       if (lse->size[a] != lsz[a])
         return fail(FL_ERR_SHAPE, "lse size[%d] = %lld, expected %lld", a, (long long)lse->size[a], (long long)lsz[a]);
   }
+  if (weights != nullptr && !empty && (st = fl::host::check_weights(weights, "weights", B, Hkv, kv->max_seq_len)) != FL_OK) return st;
   if (empty) return FL_OK;
   if (aux == nullptr) return fail(FL_ERR_AUX_MISSING, "the decode step needs aux (workspace)");
   if (desc->score_mod == FL_MOD_ALIBI && aux->alibi_slopes == nullptr) return fail(FL_ERR_AUX_MISSING, "alibi_slopes");
-  const size_t ws_need = (size_t)(B * T * H * ns) * (size_t)(D + 2) * sizeof(float);
+  const size_t ws_need = weights != nullptr ? decode_partial_bytes(B, T, H, D, ns) + decode_score_bytes(B, T, H, kv->max_seq_len)
+                                            : (size_t)(B * T * H * ns) * (size_t)(D + 2) * sizeof(float);
   if (aux->workspace == nullptr || aux->workspace_bytes < ws_need)
     return fail(FL_ERR_WORKSPACE, "workspace needs %zu bytes, got %zu", ws_need, aux->workspace ? aux->workspace_bytes : (size_t)0);
   if (((uintptr_t)aux->workspace) % 16 != 0) return fail(FL_ERR_ALIGN, "workspace not 16-byte aligned");
-  if (B * Hkv * ns > 0x7fffffffLL || B * T * H > 0x7fffffffLL) return fail(FL_ERR_SHAPE, "too many workgroups");
+  const int64_t weight_blocks = weights != nullptr ? (kv->max_seq_len + 255LL) / 256 : 0;
+  if (B * Hkv * ns > 0x7fffffffLL || B * T * H + B * Hkv * weight_blocks > 0x7fffffffLL) return fail(FL_ERR_SHAPE, "too many workgroups");
 
   fl::DecodeParams p;
   memset(&p, 0, sizeof(p));
@@ -2402,11 +2392,37 @@ fl_status fl_attn_decode(const fl_tensor* q, const fl_tensor* k_cache, const fl_
   p.scale = desc->scale;
   p.softcap = desc->softcap;
   hipStream_t stream = (hipStream_t)stream_v;
+  if (weights != nullptr) {
+    p.weights = (float*)weights->ptr;
+    p.w_sb = B > 1 ? weights->stride[0] : 0;
+    p.w_sh = Hkv > 1 ? weights->stride[2] : 0;
+    p.scores = (float*)((char*)aux->workspace + decode_partial_bytes(B, T, H, D, ns));
+    p.score_tiles = (int)((kv->max_seq_len + 31LL) / 32);
+    p.weight_blocks = (int)weight_blocks;
+    p.by_blocks = fl::Divisor::of(weight_blocks);
+  }
   hipError_t e = de->main(p, (int)(B * Hkv * ns), stream);
   if (e != hipSuccess) return fail(FL_ERR_LAUNCH, "decode launch: %s", hipGetErrorString(e));
+  if (weights != nullptr) {                        // (a single split has written the result itself: the weights alone)
+    const int64_t blocks = B * Hkv * weight_blocks + (ns > 1 ? B * T * H : 0);
+    if (blocks > 0 && (e = de->combine(p, (int)blocks, stream)) != hipSuccess) return fail(FL_ERR_LAUNCH, "decode weights launch: %s", hipGetErrorString(e));
+    return FL_OK;
+  }
   if (ns > 1 && (e = de->combine(p, (int)(B * T * H), stream)) != hipSuccess)   // a single split writes the result itself
     return fail(FL_ERR_LAUNCH, "decode merge launch: %s", hipGetErrorString(e));
   return FL_OK;
+}
+
+fl_status fl_attn_decode(const fl_tensor* q, const fl_tensor* k_cache, const fl_tensor* v_cache, const fl_paged_kv* kv,
+                         const fl_variant_desc* desc, const fl_aux* aux, fl_tensor* out, fl_tensor* lse, void* stream) {
+  return decode_call(q, k_cache, v_cache, kv, desc, aux, out, lse, nullptr, stream);
+}
+
+fl_status fl_attn_decode_weights(const fl_tensor* q, const fl_tensor* k_cache, const fl_tensor* v_cache, const fl_paged_kv* kv,
+                                 const fl_variant_desc* desc, const fl_aux* aux, fl_tensor* out, fl_tensor* lse, fl_tensor* weights,
+                                 void* stream) {
+  if (weights == nullptr) return fail(FL_ERR_NULL, "weights is NULL");
+  return decode_call(q, k_cache, v_cache, kv, desc, aux, out, lse, weights, stream);
 }
 
 // Chunks of so few rows that all (query row, head) pairs of a kv head fit the columns of the decode kernels go

@@ -40,20 +40,27 @@ struct DecodeParams {
   float* part_o;                   // workspace [B, T, H, nsplit, D]
   float* part_ml;                  // workspace [B, T, H, nsplit, 2]: running max (log2 domain), sum
   const float* alibi_slopes;       // [H]
+  // weights of the keys (fl_attn_decode_weights), or null
+  float* weights;                  // [B, Hkv, C]
+  int64_t w_sb, w_sh;
+  float* scores;                   // workspace [B * Hkv, tiles of max_len, T * H / Hkv pairs, 32 keys]: log2 domain, -inf where hidden
+  int32_t score_tiles, weight_blocks;   // tiles of a (sequence, kv head) there; workgroups of 256 keys that its weights take
   int32_t B, H, Hkv, nsplit;
   int32_t T;                       // query rows per sequence: the tokens at positions len - T .. len - 1
   int32_t num_pages;               // size[0] of the caches: table entries are cut to [0, num_pages)
   int32_t max_len;                 // the host-side bound of seq_lens that sized the launch, the table and the workspace
   int32_t window;                  // < 0: no window
   float scale, softcap;
-  Divisor by_split, by_hkv, by_group, by_h, by_t;   // nsplit, Hkv, H / Hkv, H, T: the lengths, the pages and the tiles are loads one after the other behind them
+  Divisor by_split, by_hkv, by_group, by_h, by_t, by_blocks;   // nsplit, Hkv, H / Hkv, H, T, weight_blocks: the lengths, the pages and the tiles are loads one after the other behind them
 };
 
 // Waves per workgroup where the launch has a workgroup per CU at most, or a workgroup enough tiles for them (decode_waves() chooses)
 constexpr int decode_full_waves(int D, int CB) { return D == 128 ? (CB == 1 ? 5 : 4) : 8; }
 
-template <int D_, int MOD_, int CB_ = 1, int NWV_ = decode_full_waves(D_, CB_)>
+// WEIGHTS: the scores stay behind in the workspace, for the weight that each key receives
+template <int D_, int MOD_, int CB_ = 1, int NWV_ = decode_full_waves(D_, CB_), bool WEIGHTS_ = false>
 struct DecodeCfg : BwdCfg<D_, MOD_, 0, 32, 1> {
+  static constexpr bool WEIGHTS = WEIGHTS_;
   static constexpr int CB = CB_;                   // blocks of 32 (query row, head) columns per kv head
   // D = 128: five waves with 16 KiB stages, which fill the CU's 160 KiB of LDS (four, one per SIMD, moved 4 % fewer
   // bytes per second; three waves with three stages each -- more bytes in flight per wave, fewer waves -- 15 % fewer;
@@ -258,6 +265,14 @@ decode_kernel(const DecodeParams p) {
         x[r] = a;
         mx = fmaxf(mx, a);
       }
+      if constexpr (C::WEIGHTS) {
+        // four keys a store; the live lanes of a tile fill whole lines together
+        if (live[cb]) {
+          float* at = p.scores + (((int64_t)bhk * p.score_tiles + t) * ncol + 32 * cb + w.col) * 32 + 4 * w.half;
+#pragma unroll
+          for (int g = 0; g < 4; ++g) *(float4*)(at + 8 * g) = make_float4(x[4 * g], x[4 * g + 1], x[4 * g + 2], x[4 * g + 3]);
+        }
+      }
       mx = half_swap_max(mx);
       // the running max only advances when the tile's max exceeds it by more than 2^8 (P stays
       // bounded by 2^8; l and the final division use the same reference, so nothing changes in real
@@ -343,8 +358,8 @@ decode_kernel(const DecodeParams p) {
       else *(uint2*)((uint16_t*)p.out + ob + ch) = make_uint2(pack_bf16(x.x * inv, x.y * inv), pack_bf16(x.z * inv, x.w * inv));
     }
     if (wave == 0 && w.half == 0 && live[cb]) {
-      if (!result) *(float2*)(p.part_ml + slot * 2) = make_float2(m_all, l_all);
-      else if (p.lse != nullptr)
+      if (C::WEIGHTS || !result) *(float2*)(p.part_ml + slot * 2) = make_float2(m_all, l_all);
+      if (result && p.lse != nullptr)
         p.lse[b * p.lse_sb + hq[cb] * p.lse_sh + row[cb] * p.lse_st] = l_all > 0.f ? (m_all + __log2f(l_all)) * kLn2 : -INFINITY;
     }
   }
@@ -357,8 +372,7 @@ decode_kernel(const DecodeParams p) {
 // (one sequence of 1500 - 2000 tokens, 32 / 8 heads, D = 64, 15 splits: the step 10.0 -> 9.3 us, D = 128 11.6 -> 11.1; before, the statistics were
 // read twice, then the outputs eight at a time)
 template <int D>
-__global__ void __launch_bounds__(64) decode_combine_kernel(const DecodeParams p) {
-  const int bh = blockIdx.x;                       // (b * T + row) * H + h, the order of the partial results
+__device__ __forceinline__ void decode_combine(const DecodeParams& p, const int bh) {   // bh: (b * T + row) * H + h, the order of the partial results
   const int lane = threadIdx.x, ns = p.nsplit;
   constexpr int LPR = D / 4, SPL = 64 / LPR, NL = 32 / SPL;   // lanes per row, splits per load, loads for 32 splits
   const float2* ml = (const float2*)p.part_ml + (int64_t)bh * ns;
@@ -417,6 +431,55 @@ __global__ void __launch_bounds__(64) decode_combine_kernel(const DecodeParams p
   }
   if (lane == 0 && p.lse != nullptr)
     p.lse[b * p.lse_sb + h * p.lse_sh + row * p.lse_st] = l_all > 0.f ? (m_all + __log2f(l_all)) * kLn2 : -INFINITY;
+}
+template <int D>
+__global__ void __launch_bounds__(64) decode_combine_kernel(const DecodeParams p) {
+  decode_combine<D>(p, blockIdx.x);
+}
+
+// The merge, and beside it the weight that each key has received: P = 2^(score - lse) of the scores left in the workspace, summed over the
+// kv head's (row, head) pairs, 256 keys a wave.  A pair's final statistics come from its splits', one pair per lane.
+// Reads 4 bytes per score and 8 per weight; in one launch, for both wait for the same kernel and neither fills the chip.
+template <int D>
+__global__ void __launch_bounds__(64) decode_finish_kernel(const DecodeParams p) {
+  const int n_weight_blocks = p.B * p.Hkv * p.weight_blocks;
+  if ((int)blockIdx.x >= n_weight_blocks) {
+    decode_combine<D>(p, blockIdx.x - n_weight_blocks);
+    return;
+  }
+  const int lane = threadIdx.x;
+  int bhk, blk, b, hk;
+  p.by_blocks.split(blockIdx.x, bhk, blk);
+  p.by_hkv.split(bhk, b, hk);
+  const int len = min(max(p.seq_lens[b], 0), p.max_len);
+  if (blk * 256 >= len) return;
+  const int group = (int)p.by_group.d, ncol = p.T * group;
+  // log2-domain lse of pair `lane`; +inf where the row sees no key, which makes its probabilities zero
+  float lse2 = INFINITY;
+  if (lane < ncol) {
+    int row, head;
+    p.by_group.split(lane, row, head);
+    const float2* ml = (const float2*)p.part_ml + (((int64_t)b * p.T + row) * p.H + hk * group + head) * p.nsplit;
+    float m_all = -INFINITY, l_all = 0.f;
+    for (int s = 0; s < p.nsplit; ++s) m_all = fmaxf(m_all, ml[s].x);
+    const float m_safe = m_all == -INFINITY ? 0.f : m_all;
+    for (int s = 0; s < p.nsplit; ++s) l_all = fmaf(ml[s].y, fast_exp2(ml[s].x - m_safe), l_all);
+    if (l_all > 0.f || l_all != l_all) lse2 = m_all + __log2f(l_all);
+  }
+  const int first_key = p.window >= 0 ? max(0, len - p.T - p.window) : 0;      // tiles before this key's have left no scores
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int j = blk * 256 + i * 64 + lane, t = j >> 5;
+    if (j >= len) break;
+    float gained = 0.f;
+    if (t >= first_key >> 5) {
+      const float* at = p.scores + ((int64_t)bhk * p.score_tiles + t) * ncol * 32 + (j & 31);
+      for (int c = 0; c < ncol; ++c)
+        gained += fast_exp2(at[c * 32] - __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(lse2), c)));
+    }
+    float* w = p.weights + b * p.w_sb + hk * p.w_sh + j;
+    *w = (j < len - p.T ? *w : 0.f) + gained;
+  }
 }
 
 }  // namespace fl

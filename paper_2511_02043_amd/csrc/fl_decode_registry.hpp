@@ -9,7 +9,8 @@ typedef hipError_t (*DecodeLaunchFn)(const DecodeParams& p, int nblocks, hipStre
 
 struct DecodeEntry {
   int D, mod, cb, waves;          // cb: blocks of 32 (query row, head) columns per kv head; waves of a workgroup
-  DecodeLaunchFn main, combine;   // main: B * Hkv * nsplit workgroups; combine: B * T * H workgroups
+  bool weights;                   // leaves the scores behind for the keys' weights; combine then is the kernel that forms these, too
+  DecodeLaunchFn main, combine;   // main: B * Hkv * nsplit workgroups; combine: B * T * H workgroups, behind those of the weights
 };
 
 template <class C>
@@ -26,11 +27,22 @@ hipError_t launch_decode_combine(const DecodeParams& p, int nblocks, hipStream_t
   return hipGetLastError();
 }
 
+template <int D>
+hipError_t launch_decode_finish(const DecodeParams& p, int nblocks, hipStream_t stream) {
+  hipLaunchKernelGGL(decode_finish_kernel<D>, dim3(nblocks), dim3(64), 0, stream, p);
+  return hipGetLastError();
+}
+
 template <int D, int MOD, int CB = 1, int WAVES = decode_full_waves(D, CB)>
 constexpr DecodeEntry decode_entry() {
-  return DecodeEntry{D, MOD, CB, WAVES, &launch_decode<DecodeCfg<D, MOD, CB, WAVES>>, &launch_decode_combine<D>};
+  return DecodeEntry{D, MOD, CB, WAVES, false, &launch_decode<DecodeCfg<D, MOD, CB, WAVES>>, &launch_decode_combine<D>};
+}
+template <int D, int MOD, int CB = 1, int WAVES = decode_full_waves(D, CB)>
+constexpr DecodeEntry decode_weights_entry() {
+  return DecodeEntry{D, MOD, CB, WAVES, true, &launch_decode<DecodeCfg<D, MOD, CB, WAVES, true>>, &launch_decode_finish<D>};
 }
 
 const DecodeEntry* entries_decode(int* n);
+const DecodeEntry* entries_decode_weights(int* n);
 
 }  // namespace fl

@@ -1,6 +1,7 @@
 // Host-side helpers shared by the translation units that implement the C ABI: the thread-local
 // error detail, and the checks / views of [B, G, H, S, D] tensors.
 #pragma once
+#include <cmath>
 #include <cstdarg>
 #include <cstdint>
 #include <cstdio>
@@ -23,6 +24,39 @@ inline fl_status fail(fl_status st, const char* fmt, ...) {
 }
 
 
+// A window that reaches past both sequence ends changes nothing; cutting it there keeps the kernels'
+// int32 arithmetic on i - window and j + window far from overflow (callers pass INT_MAX for "no limit").
+inline int32_t clamp_window(int32_t window, int64_t Sq, int64_t Sk) {
+  const int64_t lim = Sq > Sk ? Sq : Sk;
+  return (int64_t)window > lim ? (int32_t)lim : window;
+}
+
+// Canonical mask bits: WINDOW implies CAUSAL.
+inline uint32_t canonical_mask(uint32_t m) { return (m & FL_MASK_WINDOW) ? (m | FL_MASK_CAUSAL) : m; }
+
+inline fl_status check_desc(const fl_variant_desc* d) {
+  if (d == nullptr) return fail(FL_ERR_NULL, "desc is NULL");
+  if (d->struct_size != sizeof(fl_variant_desc))
+    return fail(FL_ERR_DESC, "desc->struct_size = %u, expected %zu", d->struct_size, sizeof(fl_variant_desc));
+  if (!(d->scale > 0.f) || !std::isfinite(d->scale)) return fail(FL_ERR_DESC, "scale must be finite and > 0");
+  if (d->score_mod > FL_MOD_SOFTCAP) return fail(FL_ERR_DESC, "unknown score_mod %u", d->score_mod);
+  if (d->score_mod == FL_MOD_SOFTCAP && (!(d->softcap > 0.f) || !std::isfinite(d->softcap)))
+    return fail(FL_ERR_DESC, "softcap must be finite and > 0");
+  if (d->mask & ~(uint32_t)(FL_MASK_CAUSAL | FL_MASK_WINDOW | FL_MASK_DOC | FL_MASK_PREFIX))
+    return fail(FL_ERR_DESC, "unknown mask bits 0x%x", d->mask);
+  if ((d->mask & FL_MASK_PREFIX) && (d->mask & (FL_MASK_CAUSAL | FL_MASK_WINDOW)))
+    return fail(FL_ERR_DESC, "FL_MASK_PREFIX excludes FL_MASK_CAUSAL and FL_MASK_WINDOW");
+  if ((d->mask & FL_MASK_WINDOW) && d->window < 0) return fail(FL_ERR_DESC, "window must be >= 0");
+  if ((d->mask & FL_MASK_PREFIX) && d->prefix_len < 0) return fail(FL_ERR_DESC, "prefix_len must be >= 0");
+  if (d->n_bias > 2) return fail(FL_ERR_DESC, "n_bias must be 0..2");
+  if (d->combine > FL_DIFFERENTIAL) return fail(FL_ERR_DESC, "unknown combine %u", d->combine);
+  if (d->epilogue & ~(uint32_t)(FL_EPI_RMSNORM | FL_EPI_GATE_SIGMOID))
+    return fail(FL_ERR_DESC, "unknown epilogue bits 0x%x", d->epilogue);
+  if ((d->epilogue & FL_EPI_RMSNORM) && (!(d->rms_eps >= 0.f) || !std::isfinite(d->rms_eps)))
+    return fail(FL_ERR_DESC, "rms_eps must be finite and >= 0");
+  if (d->q_offset < 0 || d->q_offset > 0x3fffffff) return fail(FL_ERR_DESC, "q_offset must be in [0, 2^30)");
+  return FL_OK;
+}
 
 inline int elem_size(int dtype) { return dtype == FL_BF16 ? 2 : 4; }
 
@@ -59,6 +93,56 @@ inline fl::View make_view(const fl_tensor* t) {
   return v;
 }
 
+// The accumulated weights of cached keys, [B, 1, Hkv, 1, C] f32 with C >= least.
+inline fl_status check_weights(const fl_tensor* t, const char* name, int64_t B, int64_t Hkv, int64_t least) {
+  if (t == nullptr || t->ptr == nullptr) return fail(FL_ERR_NULL, "%s is NULL", name);
+  if (t->dtype != FL_F32) return fail(FL_ERR_DTYPE, "%s must be f32", name);
+  const int64_t want[4] = {B, 1, Hkv, 1};
+  for (int a = 0; a < 4; ++a)
+    if (t->size[a] != want[a])
+      return fail(FL_ERR_SHAPE, "%s size[%d] = %lld, expected %lld", name, a, (long long)t->size[a], (long long)want[a]);
+  if (t->size[4] < least)
+    return fail(FL_ERR_SHAPE, "%s has %lld slots per head, %lld needed", name, (long long)t->size[4], (long long)least);
+  if (t->size[4] > 0x7fffffffLL) return fail(FL_ERR_SHAPE, "%s has more slots than an int32 can count", name);
+  if (t->stride[4] != 1) return fail(FL_ERR_STRIDE, "%s innermost stride must be 1", name);
+  if (((uintptr_t)t->ptr) % 4 != 0) return fail(FL_ERR_ALIGN, "%s base pointer not 4-byte aligned", name);
+  for (int a = 0; a < 4; a += 2)
+    if (t->size[a] > 1 && t->stride[a] < t->size[4]) return fail(FL_ERR_STRIDE, "%s stride[%d]: rows overlap", name, a);
+  return FL_OK;
+}
+
+// The caches [pages, 1, Hkv, page_size, D] bf16 that fl_paged_kv speaks of, B sequences of which are used.  page_shift: log2 of the page size
+// (0 where it is no power of two, which only a cache without a block table may have).
+inline fl_status check_cache(const fl_paged_kv* kv, const fl_tensor* k_cache, const fl_tensor* v_cache, int64_t B, int64_t Hkv, int64_t D,
+                             int* page_shift) {
+  if (kv == nullptr || k_cache == nullptr) return fail(FL_ERR_NULL, "kv or k_cache is NULL");
+  if (kv->struct_size != sizeof(fl_paged_kv)) return fail(FL_ERR_DESC, "kv->struct_size = %u, expected %zu", kv->struct_size, sizeof(fl_paged_kv));
+  const int64_t pages = k_cache->size[0], page_size = k_cache->size[3];
+  if (pages < 0 || page_size <= 0) return fail(FL_ERR_SHAPE, "negative size");
+  if (pages > 0x7fffffffLL) return fail(FL_ERR_SHAPE, "more pages than an int32 table entry can name");
+  if (kv->max_seq_len < 0) return fail(FL_ERR_SHAPE, "max_seq_len negative");
+  if (pages == 0 && kv->max_seq_len > 0) return fail(FL_ERR_SHAPE, "max_seq_len = %d with an empty cache", kv->max_seq_len);
+  if (kv->page_size != page_size) return fail(FL_ERR_SHAPE, "kv->page_size = %d, cache size[3] = %lld", kv->page_size, (long long)page_size);
+  *page_shift = 0;
+  const bool power = (page_size & (page_size - 1)) == 0;
+  if (power)
+    while ((1LL << *page_shift) < page_size) ++*page_shift;
+  if (kv->block_table != nullptr) {
+    if (page_size < 8 || !power) return fail(FL_ERR_SHAPE, "with a block table the page size (%lld) must be a power of two >= 8", (long long)page_size);
+    if (kv->table_stride < (kv->max_seq_len + page_size - 1) / page_size)
+      return fail(FL_ERR_SHAPE, "table_stride %d is less than the pages of max_seq_len", kv->table_stride);
+  } else {
+    if (pages < B) return fail(FL_ERR_SHAPE, "without a block table the cache needs a page per sequence");
+    if (kv->max_seq_len > page_size) return fail(FL_ERR_SHAPE, "max_seq_len exceeds the page size");
+  }
+  if (B == 0 || Hkv == 0) return FL_OK;
+  if (kv->seq_lens == nullptr) return fail(FL_ERR_NULL, "seq_lens is NULL");
+  const int64_t size[5] = {pages, 1, Hkv, page_size, D};
+  fl_status st = FL_OK;
+  if (kv->max_seq_len > 0 && (st = check_data_tensor(k_cache, "k_cache", FL_BF16, size)) == FL_OK && v_cache != nullptr)
+    st = check_data_tensor(v_cache, "v_cache", FL_BF16, size);
+  return st;
+}
 
 }  // namespace host
 }  // namespace fl

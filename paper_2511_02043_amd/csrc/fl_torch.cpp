@@ -1,5 +1,5 @@
 // Marshalling of the PyTorch entry points (attention and its backward pass, with and without the variants' extra tensors, a decode
-// step, a chunk of a paged prefill): torch tensors in, C-ABI descriptors filled, outputs and workspace taken from torch's
+// step, a chunk of a paged prefill, rotary positions, weights of cached keys, eviction): torch tensors in, C-ABI descriptors filled, outputs and workspace taken from torch's
 // allocator, one call of libflattn.so, the fl_status and the outputs back.  No attention arithmetic and no kernel is here.
 //
 // The same in Python (ctypes structures filled field by field) cost 20 us of a 31 us causal call on [1, 8, 128, 64] and of
@@ -244,6 +244,135 @@ std::tuple<int, int64_t, Tensor, OptTensor> paged(bool decode, const Tensor& q, 
   return {status, (int64_t)need, out, lse};
 }
 
+// ---- a bounded key/value cache: positions, weights of cached keys, eviction ----
+
+fl_paged_kv paged_kv(const Tensor& cache, const Tensor& seq_lens, const OptTensor& table, int max_seq_len) {
+  fl_paged_kv kv = {};
+  kv.struct_size = sizeof(kv);
+  kv.block_table = ptr<const int32_t>(table);
+  kv.table_stride = table.has_value() ? (int32_t)table->stride(0) : 0;
+  kv.page_size = (int32_t)cache.size(1);
+  kv.seq_lens = (const int32_t*)seq_lens.data_ptr();
+  kv.max_seq_len = max_seq_len;
+  return kv;
+}
+// [B, heads, D] or [B, heads, T, D]
+fl_tensor rows_desc(const Tensor& t) { return t.dim() == 3 ? desc5(t, {0, -1, 1, -1, 2}) : desc5(t, {0, -1, 1, 2, 3}); }
+fl_tensor cache_desc(const Tensor& t) { return desc5(t, {0, -1, 2, 1, 3}); }
+
+fl_rotary rotary_desc(const Tensor& positions, const Tensor& inv_freq, const std::vector<int64_t>& sections, bool interleaved, bool inverse) {
+  fl_rotary r = {};
+  r.struct_size = sizeof(r);
+  r.axes = (uint32_t)sections.size();              // (more than four are refused by the call)
+  for (size_t a = 0; a < sections.size() && a < 4; ++a) r.sections[a] = (int32_t)sections[a];
+  r.interleaved = interleaved;
+  r.inverse = inverse;
+  r.positions = (const int32_t*)positions.data_ptr();
+  for (int a = 0; a < 3; ++a) r.stride[a] = positions.size(a) > 1 ? positions.stride(a) : 0;
+  r.inv_freq = (const float*)inv_freq.data_ptr();
+  return r;
+}
+
+// q and k [B, heads, S, D], either may be missing; the outputs have their layouts
+std::tuple<int, OptTensor, OptTensor> rotary(const OptTensor& q, const OptTensor& k, const Tensor& positions, const Tensor& inv_freq,
+                                             const std::vector<int64_t>& sections, bool interleaved, bool inverse, int64_t stream) {
+  const c10::DeviceGuard guard(positions.device());
+  const fl_rotary r = rotary_desc(positions, inv_freq, sections, interleaved, inverse);
+  OptTensor qo, ko;
+  fl_tensor tq = {}, tk = {}, tqo = {}, tko = {};
+  if (q.has_value()) {
+    qo = at::empty_like(*q);
+    tq = rows_desc(*q);
+    tqo = rows_desc(*qo);
+  }
+  if (k.has_value()) {
+    ko = at::empty_like(*k);
+    tk = rows_desc(*k);
+    tko = rows_desc(*ko);
+  }
+  const int status = fl_rotary_embed(q.has_value() ? &tq : nullptr, k.has_value() ? &tk : nullptr, &r, q.has_value() ? &tqo : nullptr,
+                                     k.has_value() ? &tko : nullptr, (void*)stream);
+  return {status, qo, ko};
+}
+
+// q [B, H, (T,) D], k and v [B, Hkv, (T,) D]: the turned q, in a layout of its own; keys and values into the caches
+std::tuple<int, Tensor> rotary_append(const Tensor& q, const Tensor& k, const Tensor& v, const Tensor& positions, const Tensor& inv_freq,
+                                      const std::vector<int64_t>& sections, bool interleaved, const Tensor& k_cache, const Tensor& v_cache,
+                                      const Tensor& seq_lens, const OptTensor& table, int max_seq_len, int64_t stream) {
+  const c10::DeviceGuard guard(q.device());
+  const fl_rotary r = rotary_desc(positions, inv_freq, sections, interleaved, false);
+  Tensor qo = at::empty_like(q);
+  const fl_tensor tq = rows_desc(q), tk = rows_desc(k), tv = rows_desc(v);
+  fl_tensor tqo = rows_desc(qo), tkc = cache_desc(k_cache), tvc = cache_desc(v_cache);
+  const fl_paged_kv kv = paged_kv(k_cache, seq_lens, table, max_seq_len);
+  const int status = fl_rotary_append(&tq, &tk, &tv, &r, &kv, &tqo, &tkc, &tvc, (void*)stream);
+  return {status, qo};
+}
+
+// paged() for a decode step (q [B, H, D] or [B, H, T, D]) that adds up the keys' weights [B, Hkv, C]
+std::tuple<int, int64_t, Tensor, OptTensor> decode_weights(const Tensor& q, const Tensor& k_cache, const Tensor& v_cache, const Tensor& weights,
+                                                           const Tensor& seq_lens, const OptTensor& table, int max_seq_len, double scale, int mod,
+                                                           double softcap, int mask, int window, const OptTensor& slopes,
+                                                           const OptTensor& workspace, bool want_lse, int64_t stream) {
+  const c10::DeviceGuard guard(q.device());
+  const fl_tensor tq = rows_desc(q), tk = cache_desc(k_cache), tv = cache_desc(v_cache);
+  Tensor out = at::empty(q.sizes(), q.options());
+  fl_tensor tout = rows_desc(out), tw = desc5(weights, {0, -1, 1, -1, 2}), tlse = {};
+  OptTensor lse;
+  if (want_lse) {
+    lse = at::empty(q.sizes().slice(0, q.dim() - 1), q.options().dtype(at::kFloat));
+    tlse = q.dim() == 3 ? desc5(*lse, {0, -1, 1, -1, -1}) : desc5(*lse, {0, -1, 1, 2, -1});
+  }
+  const fl_paged_kv kv = paged_kv(k_cache, seq_lens, table, max_seq_len);
+  const size_t need = std::max<size_t>(fl_attn_decode_weights_workspace_size(&tq, &tk, &kv), 16);
+  if (workspace.has_value() && workspace->nbytes() < need) return {0, (int64_t)need, out, lse};
+  const Tensor ws = workspace.has_value() ? *workspace : bytes(need, q);
+  const fl_variant_desc d = variant(scale, mod, softcap, mask, window, 0, 0);
+  const fl_aux a = aux_of(slopes, std::nullopt, std::nullopt, ws);
+  const int status = fl_attn_decode_weights(&tq, &tk, &tv, &kv, &d, &a, &tout, want_lse ? &tlse : nullptr, &tw, (void*)stream);
+  return {status, (int64_t)need, out, lse};
+}
+
+// The weights that a chunk's rows (q [B, H, Sq, D], lse [B, H, Sq]) give to cached keys; status and the workspace bytes needed
+std::tuple<int, int64_t> key_weights(const Tensor& q, const Tensor& k_cache, const Tensor& lse, const Tensor& weights, const Tensor& seq_lens,
+                                     const OptTensor& table, int max_seq_len, double scale, int mod, double softcap, int mask, int window,
+                                     const OptTensor& slopes, const OptTensor& workspace, int64_t stream) {
+  const c10::DeviceGuard guard(q.device());
+  const fl_tensor tq = rows_desc(q), tk = cache_desc(k_cache), tlse = desc5(lse, {0, -1, 1, 2, -1});
+  fl_tensor tw = desc5(weights, {0, -1, 1, -1, 2});
+  const fl_paged_kv kv = paged_kv(k_cache, seq_lens, table, max_seq_len);
+  const size_t need = fl_key_weights_workspace_size(&tq, &tk, &kv);
+  if (workspace.has_value() && workspace->nbytes() < need) return {0, (int64_t)need};
+  Tensor ws;
+  if (need != 0) ws = workspace.has_value() ? *workspace : bytes(need, q);
+  const fl_variant_desc d = variant(scale, mod, softcap, mask, window, 0, 0);
+  const fl_aux a = aux_of(slopes, std::nullopt, std::nullopt, ws);
+  return {fl_key_weights(&tq, &tk, &tlse, &kv, &d, &a, &tw, (void*)stream), (int64_t)need};
+}
+
+// status, new lengths [B], weights [B, Hkv, capacity] and kept slots [B, Hkv, budget]
+std::tuple<int, Tensor, Tensor, Tensor> evict(const Tensor& weights, const Tensor& k_cache, const Tensor& v_cache, const Tensor& seq_lens,
+                                              const OptTensor& table, const Tensor& dst_table, int max_seq_len, int budget, int sinks, int recent,
+                                              int64_t capacity, int64_t stream) {
+  const c10::DeviceGuard guard(weights.device());
+  const int64_t B = weights.size(0), Hkv = weights.size(1);
+  Tensor lens = at::empty({B}, seq_lens.options()), new_weights = at::empty({B, Hkv, capacity}, weights.options()),
+         kept = at::empty({B, Hkv, budget}, seq_lens.options());
+  const fl_tensor tw = desc5(weights, {0, -1, 1, -1, 2});
+  fl_tensor tk = cache_desc(k_cache), tv = cache_desc(v_cache), tn = desc5(new_weights, {0, -1, 1, -1, 2});
+  const fl_paged_kv kv = paged_kv(k_cache, seq_lens, table, max_seq_len);
+  fl_evict e = {};
+  e.struct_size = sizeof(e);
+  e.budget = budget;
+  e.sinks = sinks;
+  e.recent = recent;
+  e.dst_table = (const int32_t*)dst_table.data_ptr();
+  e.dst_stride = (int32_t)dst_table.stride(0);
+  e.new_lens = (int32_t*)lens.data_ptr();
+  e.kept = (int32_t*)kept.data_ptr();
+  return {fl_cache_evict(&tw, &tk, &tv, &kv, &e, &tn, (void*)stream), lens, new_weights, kept};
+}
+
 // ---- the autograd nodes of training calls.  A node written in Python is entered by the engine's thread under the interpreter's lock, which
 // the calling thread has just given up.  A causal forward and backward call on [1, 8, 110, 128] took 45 or 89 us with one, by where the
 // process runs, and takes 38 or 72 with these; documents and windows 3 x 32/8 x 182 61 or 97, and 49 or 84.  Calls under a transform, a
@@ -350,6 +479,60 @@ std::tuple<int, Tensor> variant_node(const Tensor& q, const Tensor& k, const Ten
   return {0, VariantNode::apply(q, k, v, q2, k2, lam, gate, bias0, bias1, rms_weight, Done{out, lse, scalars, slopes, q_ids, kv_ids})};
 }
 
+// The outputs of rotary(), taken through Function::apply unseen.
+struct Turned {
+  const OptTensor &q, &k;
+};
+// The turn by -t of what arrives; itself differentiable, the map being linear.
+struct RotaryNode : torch::autograd::Function<RotaryNode> {
+  static torch::autograd::variable_list forward(torch::autograd::AutogradContext* ctx, const OptTensor& q, const OptTensor&, const Tensor& positions,
+                                                const Tensor& inv_freq, const std::vector<int64_t>& sections, bool interleaved, bool inverse,
+                                                const Turned& turned) {
+    ctx->set_materialize_grads(false);
+    ctx->saved_data["positions"] = positions;
+    ctx->saved_data["inv_freq"] = inv_freq;
+    ctx->saved_data["sections"] = sections;
+    ctx->saved_data["how"] = std::vector<int64_t>{q.has_value(), interleaved, inverse};
+    torch::autograd::variable_list out;
+    if (turned.q.has_value()) out.push_back(*turned.q);
+    if (turned.k.has_value()) out.push_back(*turned.k);
+    return out;
+  }
+  static torch::autograd::variable_list backward(torch::autograd::AutogradContext* ctx, const torch::autograd::variable_list& grads) {
+    const auto how = ctx->saved_data["how"].toIntVector();
+    const auto sections = ctx->saved_data["sections"].toIntVector();
+    const Tensor positions = ctx->saved_data["positions"].toTensor(), inv_freq = ctx->saved_data["inv_freq"].toTensor();
+    const int first = how[0] != 0 ? 0 : 1;
+    OptTensor g[2];                                // of q and k, where one has arrived and is wanted
+    for (size_t n = 0; n < grads.size(); ++n)
+      if (grads[n].defined() && ctx->needs_input_grad(n)) g[first + n] = readable(grads[n]);
+    torch::autograd::variable_list out(8);
+    if (!g[0].has_value() && !g[1].has_value()) return out;
+    const bool inverse = how[2] == 0;
+    auto [status, q, k] = rotary(g[0], g[1], positions, inv_freq, sections, how[1] != 0, inverse, current_stream(positions));
+    if (status != 0) throw_status(status);
+    if (at::GradMode::is_enabled()) {
+      const auto t = apply(g[0], g[1], positions, inv_freq, sections, how[1] != 0, inverse, Turned{q, k});
+      if (q.has_value()) q = t[0];
+      if (k.has_value()) k = t.back();
+    }
+    if (q.has_value()) out[0] = *q;
+    if (k.has_value()) out[1] = *k;
+    return out;
+  }
+};
+
+// rotary with a node
+std::tuple<int, OptTensor, OptTensor> rotary_node(const OptTensor& q, const OptTensor& k, const Tensor& positions, const Tensor& inv_freq,
+                                                  const std::vector<int64_t>& sections, bool interleaved, bool inverse, int64_t stream) {
+  auto [status, qo, ko] = rotary(q, k, positions, inv_freq, sections, interleaved, inverse, stream);
+  if (status != 0) return {status, qo, ko};
+  const auto t = RotaryNode::apply(q, k, positions, inv_freq, sections, interleaved, inverse, Turned{qo, ko});
+  if (qo.has_value()) qo = t[0];
+  if (ko.has_value()) ko = t.back();
+  return {0, qo, ko};
+}
+
 }  // namespace
 
 PYBIND11_MODULE(_fltorch, m) {
@@ -361,6 +544,12 @@ PYBIND11_MODULE(_fltorch, m) {
   m.def("variant_bwd", &variant_bwd, nogil());
   m.def("variant_node", &variant_node, nogil());
   m.def("paged", &paged, nogil());
+  m.def("rotary", &rotary, nogil());
+  m.def("rotary_node", &rotary_node, nogil());
+  m.def("rotary_append", &rotary_append, nogil());
+  m.def("decode_weights", &decode_weights, nogil());
+  m.def("key_weights", &key_weights, nogil());
+  m.def("evict", &evict, nogil());
   m.def("set_check", [](py::object check) {
     Py_XDECREF(g_check);
     g_check = check.release().ptr();

@@ -10,6 +10,10 @@ strided views are passed as they are.
 grouped-query heads, query-position offset (the variants fl_attn_bwd covers).
 `variant_attention()`: the same plus additive biases, the sigmoid gate, RMSNorm and the differential
 second stream, differentiable in every tensor input (fl_attn_bwd_ex).
+
+Around a bounded key/value cache: `rotary()` (positions with several axes, differentiable), `rotary_append()` (the same for new tokens,
+whose keys and values enter the pages), `decode_attention_weights()` and `prefill_key_weights()` (the weight that each cached key
+receives), `evict_cache()` (the keys of most weight move to fresh pages).
 """
 from __future__ import annotations
 
@@ -344,3 +348,215 @@ def paged_prefill_attention(q: torch.Tensor, k_cache: torch.Tensor, v_cache: tor
         scale = D ** -0.5
     return _paged_call(False, q, k_cache, v_cache, seq_lens, block_table, max_seq_len, scale, window, softcap, alibi_slopes, workspace,
                        return_lse)
+
+
+# ---- a bounded key/value cache ------------------------------------------------------------------------------------------
+
+
+def _check_rotary(q, k, positions, inv_freq, sections, B: int, S: int):
+    """The positions as [B, S, axes], and the sections."""
+    if not isinstance(positions, torch.Tensor) or positions.dim() != 3:
+        raise ValueError("positions must be a tensor [B, S, axes]")
+    if positions.shape[0] == 1 and B != 1:
+        positions = positions.expand(B, -1, -1)
+    _check_aux("positions", positions, torch.int32, (B, S, positions.shape[2]), q.device, contiguous=False)
+    if not isinstance(inv_freq, torch.Tensor) or inv_freq.dim() != 1:
+        raise ValueError("inv_freq must be a tensor [pairs]")
+    _check_aux("inv_freq", inv_freq, torch.float32, (inv_freq.shape[0],), q.device)
+    sections = (inv_freq.shape[0],) if sections is None else tuple(int(n) for n in sections)
+    if len(sections) != positions.shape[2] or not 1 <= len(sections) <= 4:
+        raise ValueError(f"{len(sections)} sections for positions with {positions.shape[2]} axes (1 to 4 of both)")
+    if min(sections) < 0 or sum(sections) != inv_freq.shape[0]:
+        raise ValueError(f"sections {sections} must be >= 0 and add up to the {inv_freq.shape[0]} pairs of inv_freq")
+    if k is not None and (k.device != q.device or k.dtype != q.dtype or k.dim() != q.dim() or k.shape[0] != q.shape[0] or k.shape[2:] != q.shape[2:]):
+        raise ValueError(f"k {tuple(k.shape)} {k.dtype} does not go with q {tuple(q.shape)} {q.dtype}")
+    return positions, sections
+
+
+def _rotary_plain(q, k, how, inverse):
+    status, qo, ko = _host().rotary(q, k, *how, inverse, _stream(how[0]))
+    if status:
+        fb.check(status)
+    return qo, ko
+
+
+def _readable(t):
+    """A gradient in a layout that the kernels read (autograd hands over a sum over an outer axis as a broadcast)."""
+    if t is None or (t.stride(-1) == 1 and t.data_ptr() % 16 == 0 and all(
+            n == 1 or (st != 0 and st * t.element_size() % 16 == 0) for n, st in zip(t.shape[:-1], t.stride()[:-1]))):
+        return t
+    return t.contiguous() if not t.is_contiguous() else t.clone()
+
+
+class _Rotary(torch.autograd.Function):
+    """rotary() where transforms, traces or torch.compile look into the node; the turn back is the same node."""
+
+    @staticmethod
+    def forward(ctx, q, k, positions, inv_freq, sections, interleaved, inverse):
+        ctx.how, ctx.inverse = (positions, inv_freq, sections, interleaved), inverse
+        return _rotary_plain(q, k, ctx.how, inverse)
+
+    @staticmethod
+    def backward(ctx, dq, dk):
+        dq, dk = (_readable(g) if need else None for g, need in zip((dq, dk), ctx.needs_input_grad))
+        if dq is None and dk is None:
+            return (None,) * 7
+        return _Rotary.apply(dq, dk, *ctx.how, not ctx.inverse) + (None,) * 5
+
+
+def rotary(q: torch.Tensor, k: Optional[torch.Tensor], positions: torch.Tensor, inv_freq: torch.Tensor, *, sections=None,
+           interleaved: bool = False):
+    """Rotary positions: channel pair i of every row turns by positions[b, s, axis of i] * inv_freq[i] (fl_rotary_embed).
+
+    q [B, H, S, D] and k [B, Hkv, S, D] (or None), bf16 or float32 on the GPU, any strides with unit inner stride; positions int32
+    [B, S, axes] ([1, S, axes] for all sequences alike), up to four axes such as time, height and width; inv_freq float32 [pairs],
+    2 * pairs <= D.  sections: the pairs of each axis, in order (None: one axis).  Pair i is the channels (i, i + pairs), or
+    (2i, 2i + 1) with interleaved; channels from 2 * pairs on stay.  Returns the turned q and k, in their layouts; differentiable
+    (any number of times) in both."""
+    if not q.is_cuda or q.dtype not in (torch.bfloat16, torch.float32) or q.dim() != 4:
+        raise ValueError("rotary() takes a bf16 or float32 CUDA q of shape [B, H, S, D] (there is no CPU or fallback path)")
+    positions, sections = _check_rotary(q, k, positions, inv_freq, sections, q.shape[0], q.shape[2])
+    how = (positions, inv_freq, sections, bool(interleaved))
+    node = _node_for((q, k))
+    if node == _NO_NODE:
+        return _rotary_plain(q, k, how, False)
+    if node == _NATIVE_NODE:
+        status, qo, ko = _host().rotary_node(q, k, *how, False, _stream(q))
+        if status:
+            fb.check(status)
+        return qo, ko
+    return _Rotary.apply(q, k, *how, False)
+
+
+def _check_cache(q, k_cache, v_cache, seq_lens, block_table, max_seq_len):
+    """The host-side bound of the lengths, after the checks that every call over the paged cache makes."""
+    for name, c in (("k_cache", k_cache), ("v_cache", v_cache)):
+        if c is not None and (c.dim() != 4 or c.dtype != torch.bfloat16 or c.device != q.device):
+            raise ValueError(f"{name} must be a bf16 tensor [pages, page_size, Hkv, D] on {q.device}")
+    if v_cache is not None and v_cache.shape != k_cache.shape:
+        raise ValueError("k_cache and v_cache must have one shape")
+    B = q.shape[0]
+    _check_aux("seq_lens", seq_lens, torch.int32, (B,), q.device)
+    if block_table is not None:
+        if block_table.dim() != 2:
+            raise ValueError("block_table must be [B, max_pages]")
+        _check_aux("block_table", block_table, torch.int32, (B, block_table.shape[1]), q.device, contiguous=False, inner_unit=True)
+    if max_seq_len is None:
+        max_seq_len = (block_table.shape[1] if block_table is not None else 1) * k_cache.shape[1]
+    elif block_table is not None and max_seq_len > block_table.shape[1] * k_cache.shape[1]:
+        raise ValueError(f"max_seq_len = {max_seq_len} is more than the {block_table.shape[1]} pages of block_table hold")
+    return int(max_seq_len)
+
+
+def rotary_append(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, positions: torch.Tensor, inv_freq: torch.Tensor, k_cache: torch.Tensor,
+                  v_cache: torch.Tensor, seq_lens: torch.Tensor, block_table: Optional[torch.Tensor] = None, *,
+                  max_seq_len: Optional[int] = None, sections=None, interleaved: bool = False) -> torch.Tensor:
+    """rotary() for the newest T tokens of every sequence in serving (fl_rotary_append): returns the turned q; the turned keys and the
+    values enter the paged cache at slots seq_lens - T .. seq_lens - 1, as decode_attention() and paged_prefill_attention() read them.
+
+    q [B, H, T, D] with k, v [B, Hkv, T, D], or without the T axis for one token; bf16.  positions int32 [B, T, axes]: where the tokens
+    are in their sequences, which after an eviction is not their slot.  Caches, seq_lens, block_table, max_seq_len as for
+    decode_attention(); tokens at negative slots and table entries that name no page are passed over.  Not differentiable."""
+    if not q.is_cuda or q.dtype != torch.bfloat16 or q.dim() not in (3, 4):
+        raise ValueError("rotary_append() takes a bf16 CUDA q of shape [B, H, T, D] or [B, H, D]")
+    T = q.shape[2] if q.dim() == 4 else 1
+    if k.shape != v.shape or v.dtype != q.dtype or v.device != q.device or k.shape[1] != k_cache.shape[2]:
+        raise ValueError(f"k {tuple(k.shape)} and v {tuple(v.shape)} do not go with the cache {tuple(k_cache.shape)}")
+    positions, sections = _check_rotary(q, k, positions, inv_freq, sections, q.shape[0], T)
+    max_seq_len = _check_cache(q, k_cache, v_cache, seq_lens, block_table, max_seq_len)
+    status, out = _host().rotary_append(q, k, v, positions, inv_freq, sections, bool(interleaved), k_cache, v_cache, seq_lens, block_table,
+                                        max_seq_len, _stream(q))
+    if status:
+        fb.check(status)
+    return out
+
+
+def _paged_variant(q, scale, window, softcap, alibi_slopes):
+    mask = (fb.FL_MASK_WINDOW | fb.FL_MASK_CAUSAL) if window is not None else fb.FL_MASK_CAUSAL
+    return (float(q.shape[-1] ** -0.5 if scale is None else scale), _score_mod(softcap, alibi_slopes), float(softcap or 0.0), mask,
+            int(window or 0), alibi_slopes)
+
+
+def _check_weights(weights, q, k_cache):
+    if not isinstance(weights, torch.Tensor) or weights.dim() != 3:
+        raise ValueError("weights must be a tensor [B, Hkv, capacity]")
+    _check_aux("weights", weights, torch.float32, (q.shape[0], k_cache.shape[2], weights.shape[2]), q.device, contiguous=False, inner_unit=True)
+
+
+def _check_workspace(workspace, need):
+    if workspace is not None and workspace.numel() * workspace.element_size() < need:
+        raise ValueError(f"workspace holds {workspace.numel() * workspace.element_size()} bytes, {need} needed")
+
+
+def decode_attention_weights(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor, weights: torch.Tensor, seq_lens: torch.Tensor,
+                             block_table: Optional[torch.Tensor] = None, *, max_seq_len: Optional[int] = None, scale: Optional[float] = None,
+                             window: Optional[int] = None, softcap: Optional[float] = None, alibi_slopes: Optional[torch.Tensor] = None,
+                             workspace: Optional[torch.Tensor] = None, return_lse: bool = False):
+    """decode_attention() that also adds up the weight each cached key receives (fl_attn_decode_weights).
+
+    q [B, H, D] (the newest token) or [B, H, T, D] (the newest T, T * H / Hkv <= 64); weights float32 [B, Hkv, capacity], capacity >=
+    max_seq_len, updated in place: a key's weight grows by the probabilities that the rows and query heads of its kv head give it, and
+    starts at zero for the newest T tokens.  The rest as for decode_attention().  Returns out (and lse).  Not differentiable."""
+    if not q.is_cuda or q.dtype != torch.bfloat16 or q.dim() not in (3, 4):
+        raise ValueError("decode_attention_weights() takes a bf16 CUDA q of shape [B, H, D] or [B, H, T, D]")
+    max_seq_len = _check_cache(q, k_cache, v_cache, seq_lens, block_table, max_seq_len)
+    _check_weights(weights, q, k_cache)
+    _check_aux("alibi_slopes", alibi_slopes, torch.float32, (q.shape[1],), q.device)
+    status, need, out, lse = _host().decode_weights(q, k_cache, v_cache, weights, seq_lens, block_table, max_seq_len,
+                                                    *_paged_variant(q, scale, window, softcap, alibi_slopes), workspace, return_lse, _stream(q))
+    if status:
+        fb.check(status)
+    _check_workspace(workspace, need)
+    return (out, lse) if return_lse else out
+
+
+def prefill_key_weights(q: torch.Tensor, k_cache: torch.Tensor, lse: torch.Tensor, weights: torch.Tensor, seq_lens: torch.Tensor,
+                        block_table: Optional[torch.Tensor] = None, *, max_seq_len: Optional[int] = None, scale: Optional[float] = None,
+                        window: Optional[int] = None, softcap: Optional[float] = None, alibi_slopes: Optional[torch.Tensor] = None,
+                        workspace: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """Adds to `weights` (as decode_attention_weights() does) what a chunk's Sq rows give to each cached key (fl_key_weights).
+
+    q [B, H, Sq, D] and the caches, lengths and variant of a paged_prefill_attention() call, lse [B, H, Sq] what it returned with
+    return_lse.  The newest Sq tokens' weights start at zero.  Returns `weights`.  Not differentiable."""
+    if not q.is_cuda or q.dtype != torch.bfloat16 or q.dim() != 4:
+        raise ValueError("prefill_key_weights() takes a bf16 CUDA q of shape [B, H, Sq, D]")
+    max_seq_len = _check_cache(q, k_cache, None, seq_lens, block_table, max_seq_len)
+    _check_weights(weights, q, k_cache)
+    _check_aux("lse", lse, torch.float32, tuple(q.shape[:3]), q.device, contiguous=False)
+    _check_aux("alibi_slopes", alibi_slopes, torch.float32, (q.shape[1],), q.device)
+    status, need = _host().key_weights(q, k_cache, lse, weights, seq_lens, block_table, max_seq_len,
+                                       *_paged_variant(q, scale, window, softcap, alibi_slopes), workspace, _stream(q))
+    if status:
+        fb.check(status)
+    _check_workspace(workspace, need)
+    return weights
+
+
+def evict_cache(weights: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor, seq_lens: torch.Tensor, block_table: Optional[torch.Tensor],
+                dst_table: torch.Tensor, budget: int, *, sinks: int = 0, recent: int = 0, capacity: Optional[int] = None,
+                max_seq_len: Optional[int] = None):
+    """Of every sequence and kv head keeps min(seq_lens, budget) cached tokens: the first `sinks`, the newest `recent`, and of the others those
+    of the largest accumulated weight (ties: the lower slots), copied in slot order to the pages of dst_table (fl_cache_evict).
+
+    weights float32 [B, Hkv, >= max_seq_len]; caches bf16, lengths and block_table as for decode_attention(); dst_table int32
+    [B, >= budget / page_size]: pages of the same caches that no sequence of the call is read from.  Afterwards a sequence lives in its
+    dst_table pages, and its old ones are the caller's to hand out again.  Returns the new lengths int32 [B], the weights of what stays float32
+    [B, Hkv, capacity] (zero behind them; capacity >= budget, by default budget), and the kept slots int32 [B, Hkv, budget] (-1 behind
+    them).  Slots of different kv heads hold different tokens then, so that a window or ALiBi slopes no longer measure distances."""
+    if not isinstance(weights, torch.Tensor) or not weights.is_cuda or weights.dim() != 3:
+        raise ValueError("evict_cache() takes CUDA weights of shape [B, Hkv, capacity]")
+    max_seq_len = _check_cache(weights, k_cache, v_cache, seq_lens, block_table, max_seq_len)
+    _check_weights(weights, weights, k_cache)
+    if not isinstance(dst_table, torch.Tensor) or dst_table.dim() != 2:
+        raise ValueError("dst_table must be [B, pages]")
+    _check_aux("dst_table", dst_table, torch.int32, (weights.shape[0], dst_table.shape[1]), weights.device, contiguous=False, inner_unit=True)
+    if budget < 1 or dst_table.shape[1] * k_cache.shape[1] < budget:
+        raise ValueError(f"budget = {budget} with {dst_table.shape[1]} pages of {k_cache.shape[1]} tokens in dst_table")
+    capacity = budget if capacity is None else capacity
+    if capacity < budget:
+        raise ValueError(f"capacity = {capacity} is less than budget = {budget}")
+    status, new_lens, new_weights, kept = _host().evict(weights, k_cache, v_cache, seq_lens, block_table, dst_table, max_seq_len, int(budget),
+                                                        int(sinks), int(recent), int(capacity), _stream(weights))
+    if status:
+        fb.check(status)
+    return new_lens, new_weights, kept
