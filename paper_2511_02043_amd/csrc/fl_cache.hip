@@ -295,7 +295,30 @@ fl_status fl_key_weights(const fl_tensor* q, const fl_tensor* k_cache, const fl_
   return FL_OK;
 }
 
+}  // extern "C"
+
 // ---- eviction ----
+
+namespace {
+
+template <int THREADS, bool HELD>
+hipError_t launch_select(const fl::EvictParams& p, unsigned blocks, hipStream_t stream) {
+  const hipError_t e = fl::raise_lds_limit(fl::evict_select_kernel<THREADS, HELD>);
+  if (e != hipSuccess) return e;
+  const size_t lds = sizeof(fl::SelectShared) + (HELD ? (size_t)p.max_len * sizeof(float) : 0);
+  hipLaunchKernelGGL((fl::evict_select_kernel<THREADS, HELD>), dim3(blocks), dim3(THREADS), lds, stream, p);
+  return hipGetLastError();
+}
+// By the longest sequence that may come: short ones need no more than four waves, whose barriers are cheaper and of which several workgroups share
+// a compute unit.
+hipError_t launch_select(const fl::EvictParams& p, unsigned blocks, hipStream_t stream) {
+  if (p.max_len <= 4096) return launch_select<256, true>(p, blocks, stream);
+  return p.max_len <= fl::kSelectHeld ? launch_select<1024, true>(p, blocks, stream) : launch_select<1024, false>(p, blocks, stream);
+}
+
+}  // namespace
+
+extern "C" {
 
 fl_status fl_cache_evict(const fl_tensor* weights, fl_tensor* k_cache, fl_tensor* v_cache, const fl_paged_kv* kv, const fl_evict* evict,
                          fl_tensor* new_weights, void* stream_v) {
@@ -358,8 +381,7 @@ fl_status fl_cache_evict(const fl_tensor* weights, fl_tensor* k_cache, fl_tensor
   p.by_groups = fl::Divisor::of(groups);
   p.by_pieces = fl::Divisor::of(p.pieces);
   hipStream_t stream = (hipStream_t)stream_v;
-  hipLaunchKernelGGL(fl::evict_select_kernel, dim3((unsigned)(B * Hkv)), dim3(fl::kSelectThreads), 0, stream, p);
-  hipError_t e = hipGetLastError();
+  hipError_t e = launch_select(p, (unsigned)(B * Hkv), stream);
   if (e != hipSuccess) return fail(FL_ERR_LAUNCH, "eviction launch: %s", hipGetErrorString(e));
   hipLaunchKernelGGL(fl::evict_move_kernel, dim3((unsigned)(B * Hkv * groups)), dim3(256), 0, stream, p);
   if ((e = hipGetLastError()) != hipSuccess) return fail(FL_ERR_LAUNCH, "eviction copy launch: %s", hipGetErrorString(e));

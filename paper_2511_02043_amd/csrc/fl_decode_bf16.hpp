@@ -176,6 +176,9 @@ decode_kernel(const DecodeParams p) {
     for (int u = 0; u < 4; ++u) r.pg[u] = min(max(__builtin_amdgcn_readfirstlane(raw.pg[u]), 0), p.num_pages - 1);
     return r;
   };
+  // WEIGHTS: keys and values pass through the caches as data that nobody reads again (non-temporal), which leaves the scores there for the
+  // kernel behind (64 sequences of 4k - 8k tokens, 32 / 8 heads, D = 128: 372 -> 354 us, and 22.3 -> 19.6 us there)
+  constexpr int AUX = C::WEIGHTS ? 2 : 0;
   // all load instructions of tile t (32 keys of K, then of V) into ring stage `stage`; rows past
   // the sequence end repeat its last key (their scores are masked)
   auto load_tile = [&](int t, int stage, const Pages& pages) __attribute__((always_inline)) {
@@ -199,8 +202,8 @@ decode_kernel(const DecodeParams p) {
       }
       const uint16_t* kr = p.k + page * p.k_sp + off * p.k_st + hk * p.k_sh + chunk * 8;
       const uint16_t* vr = p.v + page * p.v_sp + off * p.v_st + hk * p.v_sh + chunk * 8;
-      __builtin_amdgcn_global_load_lds((global_cvoid*)kr, (lds_void*)(st + inst * 1024), 16, 0, 0);
-      __builtin_amdgcn_global_load_lds((global_cvoid*)vr, (lds_void*)(st + C::TILE + inst * 1024), 16, 0, 0);
+      __builtin_amdgcn_global_load_lds((global_cvoid*)kr, (lds_void*)(st + inst * 1024), 16, 0, AUX);
+      __builtin_amdgcn_global_load_lds((global_cvoid*)vr, (lds_void*)(st + C::TILE + inst * 1024), 16, 0, AUX);
     }
   };
 
@@ -438,8 +441,9 @@ __global__ void __launch_bounds__(64) decode_combine_kernel(const DecodeParams p
 }
 
 // The merge, and beside it the weight that each key has received: P = 2^(score - lse) of the scores left in the workspace, summed over the
-// kv head's (row, head) pairs, 256 keys a wave.  A pair's final statistics come from its splits', one pair per lane.
-// Reads 4 bytes per score and 8 per weight; in one launch, for both wait for the same kernel and neither fills the chip.
+// kv head's (row, head) pairs, 256 keys a wave.  Reads 4 bytes per score and 8 per weight; in one launch, for both wait for the same
+// kernel and neither fills the chip.  With few sequences it is a chain of memory round trips: the splits' statistics of as many pairs as
+// fit are one load, a split per lane, and the scores of four pairs are requested together, the first of them before the statistics are there.
 template <int D>
 __global__ void __launch_bounds__(64) decode_finish_kernel(const DecodeParams p) {
   const int n_weight_blocks = p.B * p.Hkv * p.weight_blocks;
@@ -447,6 +451,7 @@ __global__ void __launch_bounds__(64) decode_finish_kernel(const DecodeParams p)
     decode_combine<D>(p, blockIdx.x - n_weight_blocks);
     return;
   }
+  constexpr int KPL = 4, CU = 4;                   // keys per lane, 64 apart; pairs whose scores are in flight together
   const int lane = threadIdx.x;
   int bhk, blk, b, hk;
   p.by_blocks.split(blockIdx.x, bhk, blk);
@@ -454,32 +459,66 @@ __global__ void __launch_bounds__(64) decode_finish_kernel(const DecodeParams p)
   const int len = min(max(p.seq_lens[b], 0), p.max_len);
   if (blk * 256 >= len) return;
   const int group = (int)p.by_group.d, ncol = p.T * group;
-  // log2-domain lse of pair `lane`; +inf where the row sees no key, which makes its probabilities zero
-  float lse2 = INFINITY;
-  if (lane < ncol) {
-    int row, head;
-    p.by_group.split(lane, row, head);
-    const float2* ml = (const float2*)p.part_ml + (((int64_t)b * p.T + row) * p.H + hk * group + head) * p.nsplit;
-    float m_all = -INFINITY, l_all = 0.f;
-    for (int s = 0; s < p.nsplit; ++s) m_all = fmaxf(m_all, ml[s].x);
-    const float m_safe = m_all == -INFINITY ? 0.f : m_all;
-    for (int s = 0; s < p.nsplit; ++s) l_all = fmaf(ml[s].y, fast_exp2(ml[s].x - m_safe), l_all);
-    if (l_all > 0.f || l_all != l_all) lse2 = m_all + __log2f(l_all);
-  }
   const int first_key = p.window >= 0 ? max(0, len - p.T - p.window) : 0;      // tiles before this key's have left no scores
+  int j[KPL];
+  bool scored[KPL];
+  const float* at[KPL];
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const int j = blk * 256 + i * 64 + lane, t = j >> 5;
-    if (j >= len) break;
-    float gained = 0.f;
-    if (t >= first_key >> 5) {
-      const float* at = p.scores + ((int64_t)bhk * p.score_tiles + t) * ncol * 32 + (j & 31);
-      for (int c = 0; c < ncol; ++c)
-        gained += fast_exp2(at[c * 32] - __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(lse2), c)));
-    }
-    float* w = p.weights + b * p.w_sb + hk * p.w_sh + j;
-    *w = (j < len - p.T ? *w : 0.f) + gained;
+  for (int i = 0; i < KPL; ++i) {
+    j[i] = blk * 256 + i * 64 + lane;
+    scored[i] = j[i] < len && j[i] >> 5 >= first_key >> 5;
+    at[i] = p.scores + ((int64_t)bhk * p.score_tiles + (j[i] >> 5)) * ncol * 32 + (j[i] & 31);
   }
+  float x[CU][KPL];
+  auto load = [&](int c0) __attribute__((always_inline)) {
+#pragma unroll
+    for (int c = 0; c < CU; ++c)
+#pragma unroll
+      for (int i = 0; i < KPL; ++i) x[c][i] = c0 + c < ncol && scored[i] ? at[i][(c0 + c) * 32] : -INFINITY;
+  };
+  load(0);
+  float* w = p.weights + b * p.w_sb + hk * p.w_sh;
+  float old[KPL];
+#pragma unroll
+  for (int i = 0; i < KPL; ++i) old[i] = j[i] < len - p.T ? w[j[i]] : 0.f;
+
+  // log2-domain lse of pair c in lane c; +inf where the row sees no key, which makes its probabilities zero
+  float lse2 = INFINITY;
+  const int span = p.nsplit > 32 ? 64 : (p.nsplit > 16 ? 32 : (p.nsplit > 8 ? 16 : (p.nsplit > 4 ? 8 : 4)));   // lanes of a pair
+  const int per = 64 / span, s0 = lane & (span - 1);
+  for (int c0 = 0; c0 < ncol; c0 += per) {
+    const int c = min(c0 + lane / span, ncol - 1);
+    int row, head;
+    p.by_group.split(c, row, head);
+    const float2* ml = (const float2*)p.part_ml + (((int64_t)b * p.T + row) * p.H + hk * group + head) * p.nsplit;
+    float2 st = s0 < p.nsplit ? ml[s0] : make_float2(-INFINITY, 0.f);
+    for (int s = s0 + 64; s < p.nsplit; s += 64) {   // (more than 64 splits: only where they are asked for)
+      const float2 y = ml[s];
+      const float m = fmaxf(st.x, y.x), ref = m == -INFINITY ? 0.f : m;
+      st = make_float2(m, st.y * fast_exp2(st.x - ref) + y.y * fast_exp2(y.x - ref));
+    }
+    float m_all = st.x;
+    for (int o = span / 2; o >= 1; o >>= 1) m_all = fmaxf(m_all, __shfl_xor(m_all, o));
+    const float ref = m_all == -INFINITY ? 0.f : m_all;
+    float l_all = st.y * fast_exp2(st.x - ref);
+    for (int o = span / 2; o >= 1; o >>= 1) l_all += __shfl_xor(l_all, o);
+    const float mine = l_all > 0.f || l_all != l_all ? m_all + __log2f(l_all) : INFINITY;
+    const float of_lane = __shfl(mine, ((lane - c0) & (per - 1)) * span);
+    if (lane >= c0 && lane < c0 + per) lse2 = of_lane;
+  }
+  float gained[KPL] = {};
+  for (int c0 = 0; c0 < ncol; c0 += CU) {
+    if (c0 > 0) load(c0);
+#pragma unroll
+    for (int c = 0; c < CU; ++c) {
+      const float ref = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(lse2), min(c0 + c, ncol - 1)));
+#pragma unroll
+      for (int i = 0; i < KPL; ++i) gained[i] += c0 + c < ncol && scored[i] ? fast_exp2(x[c][i] - ref) : 0.f;
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < KPL; ++i)
+    if (j[i] < len) w[j[i]] = old[i] + gained[i];
 }
 
 }  // namespace fl

@@ -2,8 +2,10 @@
 //
 // Of every (sequence, kv head) the first `sinks` slots, the newest `recent`, and of the others the heaviest stay, `budget` in all:
 //   * evict_select_kernel, a workgroup per (sequence, kv head), finds the weight T at which the count is reached by a radix selection
-//     (four histograms of eight bits, on a key that orders floats as whole numbers), then walks the slots in order: what is above T stays,
-//     what equals T stays while it is needed, which leaves ties to the lower slots, and two prefix sums give each its place in the result;
+//     (three histograms of up to eleven bits, on a key that orders floats as whole numbers: the first digit has two bits of mantissa,
+//     since accumulated weights share few exponents and a wave's additions to one bin go one after the other), then walks the slots in
+//     order: what is above T stays, what equals T stays while it is needed, which leaves ties to the lower slots.  The weights are read once
+//     and wait in LDS;
 //   * evict_move_kernel copies the rows that stay: no row has two readers or two writers, pages of the result are pages that nothing is
 //     read from, so the copy needs no order and runs over all of them at once.
 // Bound by the copy: 8 D bytes read and written per row and kv head beside the 4 bytes of a weight.
@@ -39,13 +41,42 @@ __device__ __forceinline__ uint32_t weight_key(float w) {
   return (u & 0x80000000u) ? ~u : (u | 0x80000000u);
 }
 
-constexpr int kSelectThreads = 1024;
+constexpr int kSelectBins = 2048;                  // digits of 11, 11 and 10 bits
+constexpr int kSelectHeld = 32768;                 // slots whose weights fit into LDS beside the histograms
 
-__global__ void __launch_bounds__(kSelectThreads) evict_select_kernel(const EvictParams p) {
-  __shared__ uint32_t hist[256];
-  __shared__ uint32_t wave_sum[2][kSelectThreads / 64];
-  __shared__ uint32_t chosen[2];                   // digit, count above it
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+struct SelectShared {                              // in front of the weights that wait in LDS
+  uint32_t hist[3][kSelectBins];
+  uint32_t wave_sum[3][16], wave_ties[16], wave_sures[16];
+  uint32_t chosen[3][2];                           // digit, keys above it
+};
+
+__device__ __forceinline__ float weight_of_key(uint32_t key) {
+  return key == 0u ? __uint_as_float(0x7fc00000u) : __uint_as_float((key & 0x80000000u) ? key & 0x7fffffffu : ~key);
+}
+
+// Inclusive prefix sum over a wave, by the data paths between lanes (no trip through LDS).
+__device__ __forceinline__ uint32_t wave_prefix(uint32_t x) {
+  x += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x111, 0xf, 0xf, false);   // from 1, 2, 4, 8 lanes below in a row of 16
+  x += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x112, 0xf, 0xf, false);
+  x += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x114, 0xf, 0xf, false);
+  x += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x118, 0xf, 0xf, false);
+  x += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x142, 0xa, 0xf, false);   // row 0 -> 1, 2 -> 3: their last lane
+  x += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x143, 0xc, 0xf, false);   // rows 0, 1 -> 2, 3
+  return x;
+}
+
+// HELD: the keys wait in LDS between the walks over them, else the weights are read again.  A wave owns a run of the competing slots and walks it
+// 64 at a time, so that an order over the workgroup is an order over waves: counts in a wave are popcounts of a ballot, and only wave totals
+// cross it.  A walk is bound by instructions (64 slots of a wave are four cycles each), so its steps are short: slots that compete are a
+// range of their own, keys are formed once, and only a run's last step looks where the run ends.
+template <int THREADS, bool HELD>
+__global__ void __launch_bounds__(THREADS) evict_select_kernel(const EvictParams p) {
+  constexpr int WAVES = THREADS / 64, BPT = kSelectBins / THREADS;             // bins per thread
+  extern __shared__ __attribute__((aligned(16))) unsigned char select_lds[];
+  SelectShared& sh = *(SelectShared*)select_lds;
+  uint32_t* const held = (uint32_t*)(select_lds + sizeof(SelectShared));
+  static_assert(WAVES <= 16 && sizeof(SelectShared) + kSelectHeld * sizeof(uint32_t) <= 160 * 1024, "LDS of the selection");
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   int b, h;
   p.by_hkv.split(blockIdx.x, b, h);
   const int len = min(max(p.seq_lens[b], 0), p.max_len);
@@ -53,91 +84,103 @@ __global__ void __launch_bounds__(kSelectThreads) evict_select_kernel(const Evic
   const float* w = p.weights + b * p.w_sb + h * p.w_sh;
   float* nw = p.new_weights + b * p.nw_sb + h * p.nw_sh;
   int32_t* kept = p.kept + ((int64_t)b * p.Hkv + h) * p.budget;
-  if (h == 0 && tid == 0) p.new_lens[b] = n_keep;
-  for (int r = n_keep + tid; r < p.capacity; r += kSelectThreads) nw[r] = 0.f;
-  for (int r = n_keep + tid; r < p.budget; r += kSelectThreads) kept[r] = -1;
-  if (len <= p.budget) {                           // everything stays where it is in the order
-    for (int j = tid; j < len; j += kSelectThreads) {
-      kept[j] = j;
-      nw[j] = w[j];
-    }
-    return;
+  // sinks + recent <= budget; a sequence within its budget has no slot that competes
+  const int lo = len > p.budget ? p.sinks : len, m = len > p.budget ? len - p.recent - lo : 0;
+  const uint32_t need = len > p.budget ? (uint32_t)(p.budget - p.sinks - p.recent) : 0u;
+  const int steps = ((m + 63) / 64 + WAVES - 1) / WAVES;                       // of 64 slots, per wave
+  const int i0 = wave * steps * 64, count = min(max(m - i0, 0), steps * 64);   // this wave's run of competing slots
+  // f(index of a competing slot, its key), 64 together
+  auto walk = [&](auto&& f) __attribute__((always_inline)) {
+    auto key_at = [&](int i) __attribute__((always_inline)) { return HELD ? held[i] : weight_key(w[lo + i]); };
+    int i = i0 + lane;
+    const int whole = i0 + (count & ~63) + lane;
+#pragma unroll 4
+    for (; i < whole; i += 64) f(i, key_at(i));
+    if (i < i0 + count) f(i, key_at(i));
+  };
+  if constexpr (HELD) {                            // (a thread reads back what it has written itself)
+#pragma unroll 8
+    for (int i = i0 + lane; i < i0 + count; i += 64) held[i] = weight_key(w[lo + i]);
   }
-  // slots [lo, hi) compete for `need` places (sinks + recent <= budget < len)
-  const int lo = p.sinks, hi = len - p.recent;
-  int need = p.budget - p.sinks - p.recent;
-  uint32_t prefix = 0;
-  int more = need;                                 // places left for keys that agree with `prefix` in the digits seen
-  for (int shift = 24; shift >= 0 && need > 0; shift -= 8) {
-    for (int i = tid; i < 256; i += kSelectThreads) hist[i] = 0;
-    __syncthreads();
-    const uint32_t mask = shift == 24 ? 0u : ~0u << (shift + 8);
-    for (int j = lo + tid; j < hi; j += kSelectThreads) {
-      const uint32_t key = weight_key(w[j]);
-      if ((key & mask) == prefix) atomicAdd(&hist[(key >> shift) & 255u], 1u);
-    }
-    __syncthreads();
-    if (tid < 64) {                                // digit d: lane 63 - d / 4, so that a prefix sum over lanes counts from the top
-      const int d0 = 4 * (63 - lane);
-      const uint32_t c3 = hist[d0 + 3], c2 = hist[d0 + 2], c1 = hist[d0 + 1], c0 = hist[d0];
-      uint32_t above = c0 + c1 + c2 + c3;
-      for (int o = 1; o < 64; o <<= 1) {
-        const uint32_t x = __shfl_up(above, o);
-        if (lane >= o) above += x;
-      }
-      above -= c0 + c1 + c2 + c3;                  // keys in higher lanes' digits
-      const uint32_t want = (uint32_t)more;
-      uint32_t a = above;
-      const uint32_t c[4] = {c3, c2, c1, c0};
+  for (int i = tid; i < 3 * kSelectBins / 4; i += THREADS) ((uint4*)&sh.hist[0][0])[i] = make_uint4(0, 0, 0, 0);
+  __syncthreads();
+
+  uint32_t top = 0, more = need;                   // the digits of T found so far; places left for keys that agree with them
+  if (need > 0) {
 #pragma unroll
-      for (int u = 0; u < 4; ++u) {
-        if (a < want && a + c[u] >= want) {
-          chosen[0] = (uint32_t)(d0 + 3 - u);
-          chosen[1] = a;
-        }
-        a += c[u];
+    for (int pass = 0; pass < 3; ++pass) {
+      const int shift = pass == 0 ? 21 : (pass == 1 ? 10 : 0);
+      const uint32_t seen = pass == 0 ? 0u : (pass == 1 ? ~0u << 21 : ~0u << 10);
+      walk([&](int, uint32_t key) __attribute__((always_inline)) {
+        if (pass == 0 || (key & seen) == top) atomicAdd(&sh.hist[pass][(key >> shift) & (kSelectBins - 1)], 1u);
+      });
+      __syncthreads();
+      // thread t has the bins BPT (THREADS - 1 - t) and following, so that a prefix sum over threads counts from the top
+      const int d = BPT * (THREADS - 1 - tid);
+      uint32_t c[BPT], sum = 0;
+#pragma unroll
+      for (int u = 0; u < BPT; ++u) sum += c[u] = sh.hist[pass][d + u];
+      const uint32_t upto = wave_prefix(sum);
+      if (lane == 63) sh.wave_sum[pass][wave] = upto;
+      __syncthreads();
+      uint32_t above = upto - sum;
+#pragma unroll
+      for (int u = 0; u < WAVES; ++u)
+        if (u < wave) above += sh.wave_sum[pass][u];
+#pragma unroll
+      for (int u = BPT - 1; u >= 0; --u) {
+        if (above < more && above + c[u] >= more) sh.chosen[pass][0] = (uint32_t)(d + u), sh.chosen[pass][1] = above;
+        above += c[u];
       }
-    }
-    __syncthreads();
-    prefix |= chosen[0] << shift;
-    more -= (int)chosen[1];
-    __syncthreads();
-  }
-  // `prefix` is T; `more` of the keys that equal it stay
-  uint32_t ties_before = 0, kept_before = 0;
-  for (int j0 = 0; j0 < len; j0 += kSelectThreads) {
-    const int j = j0 + tid;
-    const bool in = j < len;
-    const float x = in ? w[j] : 0.f;
-    const bool competes = in && j >= lo && j < hi;
-    const uint32_t key = weight_key(x);
-    const bool tie = competes && need > 0 && key == prefix;
-    const uint64_t tie_mask = __ballot(tie);
-    if (lane == 0) wave_sum[0][wave] = __popcll(tie_mask);
-    __syncthreads();
-    uint32_t before = ties_before, all = 0;
-    for (int u = 0; u < kSelectThreads / 64; ++u) {
-      if (u < wave) before += wave_sum[0][u];
-      all += wave_sum[0][u];
-    }
-    before += __popcll(tie_mask & ((1ull << lane) - 1));
-    ties_before += all;
-    const bool stays = in && (!competes || (need > 0 && key > prefix) || (tie && before < (uint32_t)more));
-    const uint64_t stay_mask = __ballot(stays);
-    if (lane == 0) wave_sum[1][wave] = __popcll(stay_mask);
-    __syncthreads();
-    uint32_t at = kept_before, sum = 0;
-    for (int u = 0; u < kSelectThreads / 64; ++u) {
-      if (u < wave) at += wave_sum[1][u];
-      sum += wave_sum[1][u];
-    }
-    at += __popcll(stay_mask & ((1ull << lane) - 1));
-    kept_before += sum;
-    if (stays) {
-      kept[at] = j;
-      nw[at] = x;
+      __syncthreads();
+      top |= sh.chosen[pass][0] << shift;
+      more -= sh.chosen[pass][1];
     }
   }
+  // `top` is T now, and `more` of the keys that equal it stay: those in the lowest slots
+  if (need > 0) {
+    uint32_t ties = 0, sures = 0;                  // of this wave
+    walk([&](int, uint32_t key) __attribute__((always_inline)) {
+      ties += __popcll(__ballot(key == top));
+      sures += __popcll(__ballot(key > top));
+    });
+    // (the last step's lanes past the run have not counted along)
+    ties = __builtin_amdgcn_readfirstlane(ties);
+    sures = __builtin_amdgcn_readfirstlane(sures);
+    if (lane == 0) sh.wave_ties[wave] = ties, sh.wave_sures[wave] = sures;
+    __syncthreads();
+    uint32_t tie = 0, at = 0;                      // ties before this wave, and slots that stay
+#pragma unroll
+    for (int u = 0; u < WAVES; ++u)
+      if (u < wave) tie += sh.wave_ties[u], at += sh.wave_sures[u];
+    at += (uint32_t)lo + min(tie, more);
+    const uint64_t below = (1ull << lane) - 1;
+    walk([&](int i, uint32_t key) __attribute__((always_inline)) {
+      const uint64_t tie_mask = __ballot(key == top);
+      const bool stays = key > top || (key == top && tie + (uint32_t)__popcll(tie_mask & below) < more);
+      const uint64_t stay_mask = __ballot(stays);
+      if (stays) {
+        const uint32_t r = at + (uint32_t)__popcll(stay_mask & below);
+        kept[r] = lo + i;
+        nw[r] = weight_of_key(key);
+      }
+      tie += __popcll(tie_mask);
+      at += __popcll(stay_mask);
+    });
+  }
+  // what stays whatever its weight: the first slots (all, within the budget) and the newest
+  if (h == 0 && tid == 0) p.new_lens[b] = n_keep;
+  for (int j = tid; j < lo; j += THREADS) {
+    kept[j] = j;
+    nw[j] = w[j];
+  }
+  for (int r = lo + (int)need + tid; r < n_keep; r += THREADS) {
+    const int j = len - n_keep + r;
+    kept[r] = j;
+    nw[r] = w[j];
+  }
+  for (int r = n_keep + tid; r < p.budget; r += THREADS) kept[r] = -1;
+  for (int r = n_keep + tid; r < p.capacity; r += THREADS) nw[r] = 0.f;
 }
 
 // 16 bytes of a key row and of a value row per thread and step.
