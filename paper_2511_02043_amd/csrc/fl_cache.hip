@@ -282,6 +282,7 @@ fl_status fl_key_weights(const fl_tensor* q, const fl_tensor* k_cache, const fl_
   p.by_problems = fl::Divisor::of(B * Hkv);
   p.by_hkv = fl::Divisor::of(Hkv);
   p.by_kblocks = fl::Divisor::of(kblocks);
+  p.by_split = fl::Divisor::of(ns);
   hipStream_t stream = (hipStream_t)stream_v;
   const int blocks = (int)(B * Hkv * kblocks * ns);
   hipError_t e = D == 128  ? launch_key_weights<128>(desc->score_mod, p, blocks, stream)

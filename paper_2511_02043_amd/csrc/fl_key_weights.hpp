@@ -35,7 +35,7 @@ struct KeyWeightParams {
   int32_t max_len, n_kblocks, nsplit;
   int32_t window;                  // < 0: no window
   float scale, softcap;
-  Divisor by_problems, by_hkv, by_kblocks;   // B * Hkv, Hkv, n_kblocks
+  Divisor by_problems, by_hkv, by_kblocks, by_split;   // B * Hkv, Hkv, n_kblocks, nsplit
 };
 
 template <int D_, int MOD_>
@@ -59,10 +59,10 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))
   const int lane = w.lane;
 
   // problems fastest: the workgroups of one (b, hkv) go to one XCD where their number is a multiple of eight, and share its L2; early key
-  // blocks, which more rows see, first
+  // blocks, which more rows see, first, with all their parts
   int rest, bh, kb, split, b, hk;
   p.by_problems.split(blockIdx.x, rest, bh);
-  p.by_kblocks.split(rest, split, kb);
+  p.by_split.split(rest, kb, split);
   p.by_hkv.split(bh, b, hk);
   const int len = min(max(p.seq_lens[b], 0), p.max_len);
   const int k0 = kb * C::KEYS;
@@ -130,7 +130,62 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))
   int head = ld_head, tile = ld_tile;
   if (it_begin < it_end) load_item(0);
   if (it_begin + 1 < it_end) load_item(1);
+  // A block of 32 rows against the wave's keys, in flight between its products and its exponentials.  The products of one block and the
+  // exponentials of the one before are a single stream of instructions: a matrix instruction takes the unit for 32 cycles and the wave's
+  // issue for four, and what follows it in the stream runs meanwhile.
+  struct Block {
+    f32x16 s[KB];
+    i32x4 ls[4];                                   // lse of rows 8 g + 4 half + 0 .. 3
+    int p_lo;                                      // position of its first row
+    bool partial;                                  // some score is hidden (or all, of rows past the end among them)
+    float slope2;
+  };
+  Block blk[2] = {};
+  uint32_t reach[KB];                              // of a key: the window, and the positions that are left up to the sequence's last
+#pragma unroll
+  for (int n = 0; n < KB; ++n) {
+    const int left = len - 1 - (kw + 32 * n + w.col);
+    reach[n] = (uint32_t)(p.window >= 0 ? min(p.window, left) : left);
+  }
+  // exponentials of registers [R0, R1) of block o
+  auto add_up = [&](const Block& o, float (&part)[KB], auto r0c, auto r1c, auto partial) __attribute__((always_inline)) {
+    constexpr int R0 = r0c, R1 = r1c;
+    float nl[R1 - R0];
+#pragma unroll
+    for (int r = R0; r < R1; ++r) nl[r - R0] = __int_as_float(o.ls[r >> 2][r & 3]) * -kLog2e;
+#pragma unroll
+    for (int n = 0; n < KB; ++n) {
+      const int j = kw + 32 * n + w.col;
+      float x[R1 - R0];
+#pragma unroll
+      for (int r = R0; r < R1; ++r) {
+        const int pos = o.p_lo + 8 * (r >> 2) + 4 * w.half + (r & 3);
+        float a;
+        if constexpr (C::MOD == kModSoftcap) {
+          const float e = fast_exp2(o.s[n][r] * (2.f * c_scale / p.softcap));
+          a = fmaf(fast_rcp(e + 1.f), -2.f * p.softcap * kLog2e, p.softcap * kLog2e) + nl[r - R0];
+        } else if constexpr (C::MOD == kModAlibi) {
+          a = fmaf(o.s[n][r], c_scale, fmaf(-o.slope2, (float)(pos - j), nl[r - R0]));
+        } else {
+          a = fmaf(o.s[n][r], c_scale, nl[r - R0]);
+        }
+        x[r - R0] = fast_exp2(a);
+      }
+      if constexpr (partial) {
+        // row and key `gap` apart: visible from 0 to reach[n] (no branches in here; keys past the length may hold anything)
+        const int gap = o.p_lo + 4 * w.half - j;
+#pragma unroll
+        for (int r = R0; r < R1; ++r) x[r - R0] = (uint32_t)(gap + 8 * (r >> 2) + (r & 3)) <= reach[n] ? x[r - R0] : 0.f;
+      }
+#pragma unroll
+      for (int d = (R1 - R0) / 2; d >= 1; d >>= 1)
+#pragma unroll
+        for (int r = 0; r < d; ++r) x[r] += x[r + d];
+      part[n] += x[0];
+    }
+  };
   int stage = 0;
+  bool pending = false;                            // blk[1] waits for its exponentials
   for (int it = it_begin; it < it_end; ++it) {
     // this wave's part of the stage has landed (one younger stage may be in flight); behind the barrier everyone's has, and the
     // stage before is free
@@ -145,70 +200,58 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))
     if (it + 2 < it_end) load_item(stage == 0 ? 2 : stage - 1);
     const uint32_t base = (uint32_t)(stage * C::STAGE);
     const int i0 = i_lo + tile * 64;
-    const float slope2 = C::MOD == kModAlibi ? p.alibi_slopes[hk * p.group + head] * kLog2e : 0.f;
     uint32_t ra_b[KK];
 #pragma unroll
     for (int kk = 0; kk < KK; ++kk) ra_b[kk] = w.ra[kk] + base;
     static_for<0, 2>([&](auto rbc) __attribute__((always_inline)) {
       constexpr int rb = rbc;
+      Block& now = blk[rb];
+      const Block& before = blk[rb ^ 1];
       const int r0 = i0 + 32 * rb;                 // first row of the block
-      const int p_lo = first_pos + r0, p_hi = first_pos + min(r0 + 31, p.Sq - 1);   // its positions
-      // (uniform) a block past the last row, or whose rows see none of this wave's keys
-      if (r0 >= i_hi || p_hi < kw || kw >= len || (p.window >= 0 && p_lo - p.window > min(kw + 32 * KB, len) - 1)) return;
-      const bool partial = r0 + 31 >= p.Sq || p_lo < kw + 32 * KB - 1 || kw + 32 * KB > len || (p.window >= 0 && p_hi - p.window > kw);
-      // lse of rows 8 g + 4 half + 0 .. 3
-      i32x4 ls[4];
+      const int p_hi = first_pos + min(r0 + 31, p.Sq - 1);
+      now.p_lo = first_pos + r0;
+      now.partial = r0 + 31 >= p.Sq || now.p_lo < kw + 32 * KB - 1 || kw + 32 * KB > len || (p.window >= 0 && p_hi - p.window > kw);
+      now.slope2 = C::MOD == kModAlibi ? p.alibi_slopes[hk * p.group + head] * kLog2e : 0.f;
       const uint32_t ls_at = base + (uint32_t)C::TILE + rb * 128 + 16 * w.half;
-      static_for<0, 4>([&](auto g) __attribute__((always_inline)) { W::template read_b128<32 * g>(ls[g], ls_at); });
-      f32x16 s[KB];
+      static_for<0, 4>([&](auto g) __attribute__((always_inline)) { W::template read_b128<32 * g>(now.ls[g], ls_at); });
 #pragma unroll
-      for (int n = 0; n < KB; ++n) s[n] = W::zero16();
-      w.template row_stream_g<RowOne<rb * 32 * ROW>, KK, 2>([&](auto fc) __attribute__((always_inline)) {
-        return ra_b[decltype(fc)::value];
-      }, [&](auto fc, bf16x8 a) __attribute__((always_inline)) {
+      for (int n = 0; n < KB; ++n) now.s[n] = W::zero16();
+      float part[KB];
 #pragma unroll
-        for (int n = 0; n < KB; ++n) s[n] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, kf[n][decltype(fc)::value], s[n], 0, 0, 0);
-      });
-      float nl[16];
+      for (int n = 0; n < KB; ++n) part[n] = 0.f;
+      auto products = [&](auto partial) __attribute__((always_inline)) {
+        w.template row_stream_g<RowOne<rb * 32 * ROW>, KK, 2>([&](auto fc) __attribute__((always_inline)) {
+          return ra_b[decltype(fc)::value];
+        }, [&](auto fc, bf16x8 a) __attribute__((always_inline)) {
+          constexpr int f = decltype(fc)::value, RS = 16 / KK;
 #pragma unroll
-      for (int r = 0; r < 16; ++r) nl[r] = __int_as_float(ls[r >> 2][r & 3]) * -kLog2e;
+          for (int n = 0; n < KB; ++n) now.s[n] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, kf[n][f], now.s[n], 0, 0, 0);
+          add_up(before, part, std::integral_constant<int, RS * f>(), std::integral_constant<int, RS * (f + 1)>(), partial);
+        });
+      };
+      if (before.partial) products(std::true_type());
+      else products(std::false_type());
 #pragma unroll
-      for (int n = 0; n < KB; ++n) {
-        const int j = kw + 32 * n + w.col;
-        float x[16];
+      for (int g = 0; g < 4; ++g) asm volatile("" : "+v"(now.ls[g]));          // landed: not to be used further up
+      if (rb == 1 || pending) {
 #pragma unroll
-        for (int r = 0; r < 16; ++r) {
-          const int pos = p_lo + 8 * (r >> 2) + 4 * w.half + (r & 3);
-          float a;
-          if constexpr (C::MOD == kModSoftcap) {
-            const float e = fast_exp2(s[n][r] * (2.f * c_scale / p.softcap));
-            a = fmaf(fast_rcp(e + 1.f), -2.f * p.softcap * kLog2e, p.softcap * kLog2e) + nl[r];
-          } else if constexpr (C::MOD == kModAlibi) {
-            a = fmaf(s[n][r], c_scale, fmaf(-slope2, (float)(pos - j), nl[r]));
-          } else {
-            a = fmaf(s[n][r], c_scale, nl[r]);
-          }
-          x[r] = fast_exp2(a);
-        }
-        if (partial) {
-#pragma unroll
-          for (int r = 0; r < 16; ++r) {
-            const int pos = p_lo + 8 * (r >> 2) + 4 * w.half + (r & 3);
-            if (j > pos || pos >= len || (p.window >= 0 && pos - p.window > j)) x[r] = 0.f;
-          }
-        }
-#pragma unroll
-        for (int d = 8; d >= 1; d >>= 1)
-#pragma unroll
-          for (int r = 0; r < d; ++r) x[r] += x[r + d];
-        sum[n] += x[0];
+        for (int n = 0; n < KB; ++n) sum[n] += part[n];
       }
     });
+    pending = true;
     if (++tile == tiles) {
       tile = 0;
       ++head;
     }
     stage = stage == 2 ? 0 : stage + 1;
+  }
+  if (pending) {
+    float part[KB];
+#pragma unroll
+    for (int n = 0; n < KB; ++n) part[n] = 0.f;
+    add_up(blk[1], part, std::integral_constant<int, 0>(), std::integral_constant<int, 16>(), std::true_type());
+#pragma unroll
+    for (int n = 0; n < KB; ++n) sum[n] += part[n];
   }
 
 #pragma unroll
