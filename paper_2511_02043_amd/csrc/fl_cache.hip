@@ -183,7 +183,7 @@ hipError_t launch_key_weights(const fl::KeyWeightParams& p, int blocks, hipStrea
   static_assert(C::KEYS == kKeysPerBlock, "keys per workgroup");
   hipError_t e = fl::raise_lds_limit(fl::key_weights_kernel<C>);
   if (e != hipSuccess) return e;
-  hipLaunchKernelGGL(fl::key_weights_kernel<C>, dim3(blocks), dim3(256), C::LDS, stream, p);
+  hipLaunchKernelGGL(fl::key_weights_kernel<C>, dim3(blocks), dim3(C::NW * 64), C::LDS, stream, p);
   return hipGetLastError();
 }
 template <int D>
