@@ -38,7 +38,7 @@ template <>
 struct RotaryElem<uint16_t> {      // bf16
   static __device__ __forceinline__ float load(uint16_t u) { return __uint_as_float((uint32_t)u << 16); }
   static __device__ __forceinline__ uint16_t store(float x) { return __builtin_bit_cast(uint16_t, (__bf16)x); }
-  // |error| below 2^-18, a five-hundredth of what the result is rounded to
+  // the machine's sine and cosine (of whole turns); the tests hold a result to 2^-14 of its pair's length beside its own rounding of 2^-8
   static __device__ __forceinline__ void sincos_turns(float r, float& s, float& c) {
     s = __builtin_amdgcn_sinf(r);
     c = __builtin_amdgcn_cosf(r);
@@ -107,6 +107,19 @@ __global__ void __launch_bounds__(256) rotary_kernel(const RotaryParams p) {
     const bool turns = unit < turning;
     const int at0 = turns ? (INTERLEAVED ? 2 * unit * VEC : unit * VEC) : 2 * p.pairs + (unit - turning) * VEC;
     const int at1 = turns ? (INTERLEAVED ? at0 + VEC : p.pairs + at0) : at0;         // a piece that stays is read and written as both
+    Piece x0[HU], x1[HU];
+    auto load = [&](int h0) __attribute__((always_inline)) {
+#pragma unroll
+      for (int u = 0; u < HU; ++u) {
+        const int h = h0 + u;
+        if (h < h_end) {
+          const T* in = h < p.H ? q_in + h * p.q.sh : (h < p.H + p.Hkv ? k_in + (h - p.H) * p.k.sh : v_in + (h - p.H - p.Hkv) * p.v.sh);
+          x0[u] = *(const Piece*)(in + at0);
+          x1[u] = *(const Piece*)(in + at1);
+        }
+      }
+    };
+    load(h_begin);                                 // on their way while the angles are formed
     float cs[VEC], sn[VEC];
 #pragma unroll
     for (int j = 0; j < VEC; ++j) {
@@ -124,16 +137,7 @@ __global__ void __launch_bounds__(256) rotary_kernel(const RotaryParams p) {
       }
     }
     for (int h0 = h_begin; h0 < h_end; h0 += HU) {
-      Piece x0[HU], x1[HU];
-#pragma unroll
-      for (int u = 0; u < HU; ++u) {
-        const int h = h0 + u;
-        if (h < h_end) {
-          const T* in = h < p.H ? q_in + h * p.q.sh : (h < p.H + p.Hkv ? k_in + (h - p.H) * p.k.sh : v_in + (h - p.H - p.Hkv) * p.v.sh);
-          x0[u] = *(const Piece*)(in + at0);
-          x1[u] = *(const Piece*)(in + at1);
-        }
-      }
+      if (h0 > h_begin) load(h0);
 #pragma unroll
       for (int u = 0; u < HU; ++u) {
         const int h = h0 + u;

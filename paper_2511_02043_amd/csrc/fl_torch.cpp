@@ -246,6 +246,74 @@ std::tuple<int, int64_t, Tensor, OptTensor> paged(bool decode, const Tensor& q, 
 
 // ---- a bounded key/value cache: positions, weights of cached keys, eviction ----
 
+// The checks of these calls' tensors are here too: in Python they took 10 us of a 16 us call that turns one token of 64 sequences.
+template <class... Parts>
+void need(bool ok, const Parts&... parts) {
+  if (!ok) throw py::value_error(c10::str(parts...));
+}
+// an array that the C ABI reads as raw memory of a fixed type and shape
+void check_array(const char* name, const OptTensor& t, at::ScalarType dtype, at::IntArrayRef shape, at::Device device, bool contiguous, bool inner_unit) {
+  need(t.has_value(), name, " must be a torch.Tensor");
+  need(t->scalar_type() == dtype, name, " must be ", dtype, ", got ", t->scalar_type());
+  need(t->device() == device, name, " is on ", t->device(), ", expected ", device);
+  need(t->sizes() == shape, name, " must have shape ", shape, ", got ", t->sizes());
+  need(!contiguous || t->is_contiguous(), name, " must be contiguous");
+  need(!inner_unit || t->size(-1) <= 1 || t->stride(-1) == 1, name, " must have unit stride along its last axis");
+}
+typedef std::optional<std::vector<int64_t>> Sections;
+
+// The positions as [B, S, axes] and the sections, for q [B, heads, (S,) D] and k, which may be missing
+std::tuple<Tensor, std::vector<int64_t>> check_rotary(const Tensor& q, const OptTensor& k, const OptTensor& positions, const OptTensor& inv_freq,
+                                                      const Sections& given, int64_t B, int64_t S) {
+  need(positions.has_value() && positions->dim() == 3, "positions must be a tensor [B, S, axes]");
+  const int64_t axes = positions->size(2);
+  const Tensor p = positions->size(0) == 1 && B != 1 ? positions->expand({B, -1, -1}) : *positions;
+  check_array("positions", p, at::kInt, {B, S, axes}, q.device(), false, false);
+  need(inv_freq.has_value() && inv_freq->dim() == 1, "inv_freq must be a tensor [pairs]");
+  const int64_t pairs = inv_freq->size(0);
+  check_array("inv_freq", inv_freq, at::kFloat, {pairs}, q.device(), true, false);
+  std::vector<int64_t> sections = given.has_value() ? *given : std::vector<int64_t>{pairs};
+  need((int64_t)sections.size() == axes && axes >= 1 && axes <= 4, sections.size(), " sections for positions with ", axes, " axes (1 to 4 of both)");
+  int64_t sum = 0;
+  for (int64_t n : sections) {
+    need(n >= 0 && n <= pairs, "sections must be >= 0 and add up to the ", pairs, " pairs of inv_freq");
+    sum += n;
+  }
+  need(sum == pairs, "sections must be >= 0 and add up to the ", pairs, " pairs of inv_freq");
+  if (k.has_value())
+    need(k->device() == q.device() && k->scalar_type() == q.scalar_type() && k->dim() == q.dim() && k->size(0) == q.size(0) &&
+             k->sizes().slice(2) == q.sizes().slice(2),
+         "k ", k->sizes(), " ", k->scalar_type(), " does not go with q ", q.sizes(), " ", q.scalar_type());
+  return {p, std::move(sections)};
+}
+
+// The host-side bound of the lengths, after the checks that every call over the paged cache makes; q: a tensor of B sequences
+int64_t check_cache(const Tensor& q, const Tensor& k_cache, const OptTensor& v_cache, const OptTensor& seq_lens, const OptTensor& table,
+                    std::optional<int64_t> max_seq_len) {
+  for (const Tensor* c : {&k_cache, v_cache.has_value() ? &*v_cache : &k_cache})
+    need(c->dim() == 4 && c->scalar_type() == at::kBFloat16 && c->device() == q.device(), "the caches must be bf16 tensors [pages, page_size, Hkv, D] on ",
+         q.device());
+  need(!v_cache.has_value() || v_cache->sizes() == k_cache.sizes(), "k_cache and v_cache must have one shape");
+  const int64_t B = q.size(0);
+  check_array("seq_lens", seq_lens, at::kInt, {B}, q.device(), true, false);
+  if (table.has_value()) {
+    need(table->dim() == 2, "block_table must be [B, max_pages]");
+    check_array("block_table", table, at::kInt, {B, table->size(1)}, q.device(), false, true);
+  }
+  const int64_t held = (table.has_value() ? table->size(1) : 1) * k_cache.size(1), n = max_seq_len.value_or(held);
+  need(n >= 0 && n <= INT32_MAX, "max_seq_len = ", n);
+  need(!table.has_value() || n <= held, "max_seq_len = ", n, " is more than the ", table.has_value() ? table->size(1) : 1, " pages of block_table hold");
+  return n;
+}
+
+void check_weights(const OptTensor& weights, const Tensor& q, const Tensor& k_cache) {
+  need(weights.has_value() && weights->dim() == 3, "weights must be a tensor [B, Hkv, capacity]");
+  check_array("weights", weights, at::kFloat, {q.size(0), k_cache.size(2), weights->size(2)}, q.device(), false, true);
+}
+void check_slopes(const OptTensor& slopes, const Tensor& q) {
+  if (slopes.has_value()) check_array("alibi_slopes", slopes, at::kFloat, {q.size(1)}, q.device(), true, false);
+}
+
 fl_paged_kv paged_kv(const Tensor& cache, const Tensor& seq_lens, const OptTensor& table, int max_seq_len) {
   fl_paged_kv kv = {};
   kv.struct_size = sizeof(kv);
@@ -295,26 +363,41 @@ std::tuple<int, OptTensor, OptTensor> rotary(const OptTensor& q, const OptTensor
   return {status, qo, ko};
 }
 
+// ... of a call, with its checks
+std::tuple<int, OptTensor, OptTensor> rotary_checked(const Tensor& q, const OptTensor& k, const OptTensor& positions, const OptTensor& inv_freq,
+                                                     const Sections& given, bool interleaved, int64_t stream) {
+  const auto [p, sections] = check_rotary(q, k, positions, inv_freq, given, q.size(0), q.size(2));
+  return rotary(q, k, p, *inv_freq, sections, interleaved, false, stream);
+}
+
 // q [B, H, (T,) D], k and v [B, Hkv, (T,) D]: the turned q, in a layout of its own; keys and values into the caches
-std::tuple<int, Tensor> rotary_append(const Tensor& q, const Tensor& k, const Tensor& v, const Tensor& positions, const Tensor& inv_freq,
-                                      const std::vector<int64_t>& sections, bool interleaved, const Tensor& k_cache, const Tensor& v_cache,
-                                      const Tensor& seq_lens, const OptTensor& table, int max_seq_len, int64_t stream) {
+std::tuple<int, Tensor> rotary_append(const Tensor& q, const Tensor& k, const Tensor& v, const OptTensor& positions, const OptTensor& inv_freq,
+                                      const Sections& given, bool interleaved, const Tensor& k_cache, const Tensor& v_cache,
+                                      const OptTensor& seq_lens, const OptTensor& table, std::optional<int64_t> bound, int64_t stream) {
   const c10::DeviceGuard guard(q.device());
-  const fl_rotary r = rotary_desc(positions, inv_freq, sections, interleaved, false);
+  const auto [p, sections] = check_rotary(q, k, positions, inv_freq, given, q.size(0), q.dim() == 4 ? q.size(2) : 1);
+  const int max_seq_len = (int)check_cache(q, k_cache, v_cache, seq_lens, table, bound);
+  need(k.sizes() == v.sizes() && v.scalar_type() == q.scalar_type() && v.device() == q.device() && k.size(1) == k_cache.size(2), "k ", k.sizes(),
+       " and v ", v.sizes(), " do not go with the cache ", k_cache.sizes());
+  const fl_rotary r = rotary_desc(p, *inv_freq, sections, interleaved, false);
   Tensor qo = at::empty_like(q);
   const fl_tensor tq = rows_desc(q), tk = rows_desc(k), tv = rows_desc(v);
   fl_tensor tqo = rows_desc(qo), tkc = cache_desc(k_cache), tvc = cache_desc(v_cache);
-  const fl_paged_kv kv = paged_kv(k_cache, seq_lens, table, max_seq_len);
+  const fl_paged_kv kv = paged_kv(k_cache, *seq_lens, table, max_seq_len);
   const int status = fl_rotary_append(&tq, &tk, &tv, &r, &kv, &tqo, &tkc, &tvc, (void*)stream);
   return {status, qo};
 }
 
 // paged() for a decode step (q [B, H, D] or [B, H, T, D]) that adds up the keys' weights [B, Hkv, C]
-std::tuple<int, int64_t, Tensor, OptTensor> decode_weights(const Tensor& q, const Tensor& k_cache, const Tensor& v_cache, const Tensor& weights,
-                                                           const Tensor& seq_lens, const OptTensor& table, int max_seq_len, double scale, int mod,
-                                                           double softcap, int mask, int window, const OptTensor& slopes,
+std::tuple<int, int64_t, Tensor, OptTensor> decode_weights(const Tensor& q, const Tensor& k_cache, const Tensor& v_cache, const OptTensor& w,
+                                                           const OptTensor& lens, const OptTensor& table, std::optional<int64_t> bound, double scale,
+                                                           int mod, double softcap, int mask, int window, const OptTensor& slopes,
                                                            const OptTensor& workspace, bool want_lse, int64_t stream) {
   const c10::DeviceGuard guard(q.device());
+  const int max_seq_len = (int)check_cache(q, k_cache, v_cache, lens, table, bound);
+  check_weights(w, q, k_cache);
+  check_slopes(slopes, q);
+  const Tensor &weights = *w, &seq_lens = *lens;
   const fl_tensor tq = rows_desc(q), tk = cache_desc(k_cache), tv = cache_desc(v_cache);
   Tensor out = at::empty(q.sizes(), q.options());
   fl_tensor tout = rows_desc(out), tw = desc5(weights, {0, -1, 1, -1, 2}), tlse = {};
@@ -324,37 +407,51 @@ std::tuple<int, int64_t, Tensor, OptTensor> decode_weights(const Tensor& q, cons
     tlse = q.dim() == 3 ? desc5(*lse, {0, -1, 1, -1, -1}) : desc5(*lse, {0, -1, 1, 2, -1});
   }
   const fl_paged_kv kv = paged_kv(k_cache, seq_lens, table, max_seq_len);
-  const size_t need = std::max<size_t>(fl_attn_decode_weights_workspace_size(&tq, &tk, &kv), 16);
-  if (workspace.has_value() && workspace->nbytes() < need) return {0, (int64_t)need, out, lse};
-  const Tensor ws = workspace.has_value() ? *workspace : bytes(need, q);
+  const size_t room = std::max<size_t>(fl_attn_decode_weights_workspace_size(&tq, &tk, &kv), 16);
+  if (workspace.has_value() && workspace->nbytes() < room) return {0, (int64_t)room, out, lse};
+  const Tensor ws = workspace.has_value() ? *workspace : bytes(room, q);
   const fl_variant_desc d = variant(scale, mod, softcap, mask, window, 0, 0);
   const fl_aux a = aux_of(slopes, std::nullopt, std::nullopt, ws);
   const int status = fl_attn_decode_weights(&tq, &tk, &tv, &kv, &d, &a, &tout, want_lse ? &tlse : nullptr, &tw, (void*)stream);
-  return {status, (int64_t)need, out, lse};
+  return {status, (int64_t)room, out, lse};
 }
 
 // The weights that a chunk's rows (q [B, H, Sq, D], lse [B, H, Sq]) give to cached keys; status and the workspace bytes needed
-std::tuple<int, int64_t> key_weights(const Tensor& q, const Tensor& k_cache, const Tensor& lse, const Tensor& weights, const Tensor& seq_lens,
-                                     const OptTensor& table, int max_seq_len, double scale, int mod, double softcap, int mask, int window,
-                                     const OptTensor& slopes, const OptTensor& workspace, int64_t stream) {
+std::tuple<int, int64_t> key_weights(const Tensor& q, const Tensor& k_cache, const OptTensor& lse, const OptTensor& w, const OptTensor& lens,
+                                     const OptTensor& table, std::optional<int64_t> bound, double scale, int mod, double softcap, int mask,
+                                     int window, const OptTensor& slopes, const OptTensor& workspace, int64_t stream) {
   const c10::DeviceGuard guard(q.device());
-  const fl_tensor tq = rows_desc(q), tk = cache_desc(k_cache), tlse = desc5(lse, {0, -1, 1, 2, -1});
+  const int max_seq_len = (int)check_cache(q, k_cache, std::nullopt, lens, table, bound);
+  check_weights(w, q, k_cache);
+  check_array("lse", lse, at::kFloat, {q.size(0), q.size(1), q.size(2)}, q.device(), false, false);
+  check_slopes(slopes, q);
+  const Tensor &weights = *w, &seq_lens = *lens;
+  const fl_tensor tq = rows_desc(q), tk = cache_desc(k_cache), tlse = desc5(*lse, {0, -1, 1, 2, -1});
   fl_tensor tw = desc5(weights, {0, -1, 1, -1, 2});
   const fl_paged_kv kv = paged_kv(k_cache, seq_lens, table, max_seq_len);
-  const size_t need = fl_key_weights_workspace_size(&tq, &tk, &kv);
-  if (workspace.has_value() && workspace->nbytes() < need) return {0, (int64_t)need};
+  const size_t room = fl_key_weights_workspace_size(&tq, &tk, &kv);
+  if (workspace.has_value() && workspace->nbytes() < room) return {0, (int64_t)room};
   Tensor ws;
-  if (need != 0) ws = workspace.has_value() ? *workspace : bytes(need, q);
+  if (room != 0) ws = workspace.has_value() ? *workspace : bytes(room, q);
   const fl_variant_desc d = variant(scale, mod, softcap, mask, window, 0, 0);
   const fl_aux a = aux_of(slopes, std::nullopt, std::nullopt, ws);
-  return {fl_key_weights(&tq, &tk, &tlse, &kv, &d, &a, &tw, (void*)stream), (int64_t)need};
+  return {fl_key_weights(&tq, &tk, &tlse, &kv, &d, &a, &tw, (void*)stream), (int64_t)room};
 }
 
 // status, new lengths [B], weights [B, Hkv, capacity] and kept slots [B, Hkv, budget]
-std::tuple<int, Tensor, Tensor, Tensor> evict(const Tensor& weights, const Tensor& k_cache, const Tensor& v_cache, const Tensor& seq_lens,
-                                              const OptTensor& table, const Tensor& dst_table, int max_seq_len, int budget, int sinks, int recent,
-                                              int64_t capacity, int64_t stream) {
+std::tuple<int, Tensor, Tensor, Tensor> evict(const Tensor& weights, const Tensor& k_cache, const Tensor& v_cache, const OptTensor& seq,
+                                              const OptTensor& table, const OptTensor& dst, std::optional<int64_t> bound, int64_t budget, int sinks,
+                                              int recent, std::optional<int64_t> room, int64_t stream) {
   const c10::DeviceGuard guard(weights.device());
+  const int max_seq_len = (int)check_cache(weights, k_cache, v_cache, seq, table, bound);
+  check_weights(weights, weights, k_cache);
+  need(dst.has_value() && dst->dim() == 2, "dst_table must be [B, pages]");
+  check_array("dst_table", dst, at::kInt, {weights.size(0), dst->size(1)}, weights.device(), false, true);
+  need(budget >= 1 && budget <= INT32_MAX && dst->size(1) * k_cache.size(1) >= budget, "budget = ", budget, " with ", dst->size(1), " pages of ",
+       k_cache.size(1), " tokens in dst_table");
+  const int64_t capacity = room.value_or(budget);
+  need(capacity >= budget, "capacity = ", capacity, " is less than budget = ", budget);
+  const Tensor &seq_lens = *seq, &dst_table = *dst;
   const int64_t B = weights.size(0), Hkv = weights.size(1);
   Tensor lens = at::empty({B}, seq_lens.options()), new_weights = at::empty({B, Hkv, capacity}, weights.options()),
          kept = at::empty({B, Hkv, budget}, seq_lens.options());
@@ -363,7 +460,7 @@ std::tuple<int, Tensor, Tensor, Tensor> evict(const Tensor& weights, const Tenso
   const fl_paged_kv kv = paged_kv(k_cache, seq_lens, table, max_seq_len);
   fl_evict e = {};
   e.struct_size = sizeof(e);
-  e.budget = budget;
+  e.budget = (int32_t)budget;
   e.sinks = sinks;
   e.recent = recent;
   e.dst_table = (const int32_t*)dst_table.data_ptr();
@@ -522,12 +619,13 @@ struct RotaryNode : torch::autograd::Function<RotaryNode> {
   }
 };
 
-// rotary with a node
-std::tuple<int, OptTensor, OptTensor> rotary_node(const OptTensor& q, const OptTensor& k, const Tensor& positions, const Tensor& inv_freq,
-                                                  const std::vector<int64_t>& sections, bool interleaved, bool inverse, int64_t stream) {
-  auto [status, qo, ko] = rotary(q, k, positions, inv_freq, sections, interleaved, inverse, stream);
+// rotary_checked with a node
+std::tuple<int, OptTensor, OptTensor> rotary_node(const Tensor& q, const OptTensor& k, const OptTensor& positions, const OptTensor& inv_freq,
+                                                  const Sections& given, bool interleaved, int64_t stream) {
+  const auto [p, sections] = check_rotary(q, k, positions, inv_freq, given, q.size(0), q.size(2));
+  auto [status, qo, ko] = rotary(q, k, p, *inv_freq, sections, interleaved, false, stream);
   if (status != 0) return {status, qo, ko};
-  const auto t = RotaryNode::apply(q, k, positions, inv_freq, sections, interleaved, inverse, Turned{qo, ko});
+  const auto t = RotaryNode::apply(OptTensor(q), k, p, *inv_freq, sections, interleaved, false, Turned{qo, ko});
   if (qo.has_value()) qo = t[0];
   if (ko.has_value()) ko = t.back();
   return {0, qo, ko};
@@ -544,7 +642,10 @@ PYBIND11_MODULE(_fltorch, m) {
   m.def("variant_bwd", &variant_bwd, nogil());
   m.def("variant_node", &variant_node, nogil());
   m.def("paged", &paged, nogil());
+  m.def("check_rotary", &check_rotary);
+  m.def("check_cache", &check_cache);
   m.def("rotary", &rotary, nogil());
+  m.def("rotary_checked", &rotary_checked, nogil());
   m.def("rotary_node", &rotary_node, nogil());
   m.def("rotary_append", &rotary_append, nogil());
   m.def("decode_weights", &decode_weights, nogil());

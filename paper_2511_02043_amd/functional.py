@@ -355,22 +355,12 @@ def paged_prefill_attention(q: torch.Tensor, k_cache: torch.Tensor, v_cache: tor
 
 def _check_rotary(q, k, positions, inv_freq, sections, B: int, S: int):
     """The positions as [B, S, axes], and the sections."""
-    if not isinstance(positions, torch.Tensor) or positions.dim() != 3:
-        raise ValueError("positions must be a tensor [B, S, axes]")
-    if positions.shape[0] == 1 and B != 1:
-        positions = positions.expand(B, -1, -1)
-    _check_aux("positions", positions, torch.int32, (B, S, positions.shape[2]), q.device, contiguous=False)
-    if not isinstance(inv_freq, torch.Tensor) or inv_freq.dim() != 1:
-        raise ValueError("inv_freq must be a tensor [pairs]")
-    _check_aux("inv_freq", inv_freq, torch.float32, (inv_freq.shape[0],), q.device)
-    sections = (inv_freq.shape[0],) if sections is None else tuple(int(n) for n in sections)
-    if len(sections) != positions.shape[2] or not 1 <= len(sections) <= 4:
-        raise ValueError(f"{len(sections)} sections for positions with {positions.shape[2]} axes (1 to 4 of both)")
-    if min(sections) < 0 or sum(sections) != inv_freq.shape[0]:
-        raise ValueError(f"sections {sections} must be >= 0 and add up to the {inv_freq.shape[0]} pairs of inv_freq")
-    if k is not None and (k.device != q.device or k.dtype != q.dtype or k.dim() != q.dim() or k.shape[0] != q.shape[0] or k.shape[2:] != q.shape[2:]):
-        raise ValueError(f"k {tuple(k.shape)} {k.dtype} does not go with q {tuple(q.shape)} {q.dtype}")
-    return positions, sections
+    positions, sections = _host().check_rotary(q, k, positions, inv_freq, _tuple(sections), B, S)
+    return positions, tuple(sections)
+
+
+def _tuple(sections):
+    return None if sections is None else tuple(sections)
 
 
 def _rotary_plain(q, k, how, inverse):
@@ -415,37 +405,21 @@ def rotary(q: torch.Tensor, k: Optional[torch.Tensor], positions: torch.Tensor, 
     (any number of times) in both."""
     if not q.is_cuda or q.dtype not in (torch.bfloat16, torch.float32) or q.dim() != 4:
         raise ValueError("rotary() takes a bf16 or float32 CUDA q of shape [B, H, S, D] (there is no CPU or fallback path)")
-    positions, sections = _check_rotary(q, k, positions, inv_freq, sections, q.shape[0], q.shape[2])
-    how = (positions, inv_freq, sections, bool(interleaved))
+    sections = _tuple(sections)
     node = _node_for((q, k))
-    if node == _NO_NODE:
-        return _rotary_plain(q, k, how, False)
-    if node == _NATIVE_NODE:
-        status, qo, ko = _host().rotary_node(q, k, *how, False, _stream(q))
-        if status:
-            fb.check(status)
-        return qo, ko
-    return _Rotary.apply(q, k, *how, False)
+    if node == _PYTHON_NODE:
+        positions, sections = _check_rotary(q, k, positions, inv_freq, sections, q.shape[0], q.shape[2])
+        return _Rotary.apply(q, k, positions, inv_freq, sections, bool(interleaved), False)
+    call = _host().rotary_node if node == _NATIVE_NODE else _host().rotary_checked
+    status, qo, ko = call(q, k, positions, inv_freq, sections, bool(interleaved), _stream(q))
+    if status:
+        fb.check(status)
+    return qo, ko
 
 
 def _check_cache(q, k_cache, v_cache, seq_lens, block_table, max_seq_len):
     """The host-side bound of the lengths, after the checks that every call over the paged cache makes."""
-    for name, c in (("k_cache", k_cache), ("v_cache", v_cache)):
-        if c is not None and (c.dim() != 4 or c.dtype != torch.bfloat16 or c.device != q.device):
-            raise ValueError(f"{name} must be a bf16 tensor [pages, page_size, Hkv, D] on {q.device}")
-    if v_cache is not None and v_cache.shape != k_cache.shape:
-        raise ValueError("k_cache and v_cache must have one shape")
-    B = q.shape[0]
-    _check_aux("seq_lens", seq_lens, torch.int32, (B,), q.device)
-    if block_table is not None:
-        if block_table.dim() != 2:
-            raise ValueError("block_table must be [B, max_pages]")
-        _check_aux("block_table", block_table, torch.int32, (B, block_table.shape[1]), q.device, contiguous=False, inner_unit=True)
-    if max_seq_len is None:
-        max_seq_len = (block_table.shape[1] if block_table is not None else 1) * k_cache.shape[1]
-    elif block_table is not None and max_seq_len > block_table.shape[1] * k_cache.shape[1]:
-        raise ValueError(f"max_seq_len = {max_seq_len} is more than the {block_table.shape[1]} pages of block_table hold")
-    return int(max_seq_len)
+    return _host().check_cache(q, k_cache, v_cache, seq_lens, block_table, max_seq_len)
 
 
 def rotary_append(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, positions: torch.Tensor, inv_freq: torch.Tensor, k_cache: torch.Tensor,
@@ -459,12 +433,7 @@ def rotary_append(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, positions: 
     decode_attention(); tokens at negative slots and table entries that name no page are passed over.  Not differentiable."""
     if not q.is_cuda or q.dtype != torch.bfloat16 or q.dim() not in (3, 4):
         raise ValueError("rotary_append() takes a bf16 CUDA q of shape [B, H, T, D] or [B, H, D]")
-    T = q.shape[2] if q.dim() == 4 else 1
-    if k.shape != v.shape or v.dtype != q.dtype or v.device != q.device or k.shape[1] != k_cache.shape[2]:
-        raise ValueError(f"k {tuple(k.shape)} and v {tuple(v.shape)} do not go with the cache {tuple(k_cache.shape)}")
-    positions, sections = _check_rotary(q, k, positions, inv_freq, sections, q.shape[0], T)
-    max_seq_len = _check_cache(q, k_cache, v_cache, seq_lens, block_table, max_seq_len)
-    status, out = _host().rotary_append(q, k, v, positions, inv_freq, sections, bool(interleaved), k_cache, v_cache, seq_lens, block_table,
+    status, out = _host().rotary_append(q, k, v, positions, inv_freq, _tuple(sections), bool(interleaved), k_cache, v_cache, seq_lens, block_table,
                                         max_seq_len, _stream(q))
     if status:
         fb.check(status)
@@ -475,12 +444,6 @@ def _paged_variant(q, scale, window, softcap, alibi_slopes):
     mask = (fb.FL_MASK_WINDOW | fb.FL_MASK_CAUSAL) if window is not None else fb.FL_MASK_CAUSAL
     return (float(q.shape[-1] ** -0.5 if scale is None else scale), _score_mod(softcap, alibi_slopes), float(softcap or 0.0), mask,
             int(window or 0), alibi_slopes)
-
-
-def _check_weights(weights, q, k_cache):
-    if not isinstance(weights, torch.Tensor) or weights.dim() != 3:
-        raise ValueError("weights must be a tensor [B, Hkv, capacity]")
-    _check_aux("weights", weights, torch.float32, (q.shape[0], k_cache.shape[2], weights.shape[2]), q.device, contiguous=False, inner_unit=True)
 
 
 def _check_workspace(workspace, need):
@@ -499,9 +462,6 @@ def decode_attention_weights(q: torch.Tensor, k_cache: torch.Tensor, v_cache: to
     starts at zero for the newest T tokens.  The rest as for decode_attention().  Returns out (and lse).  Not differentiable."""
     if not q.is_cuda or q.dtype != torch.bfloat16 or q.dim() not in (3, 4):
         raise ValueError("decode_attention_weights() takes a bf16 CUDA q of shape [B, H, D] or [B, H, T, D]")
-    max_seq_len = _check_cache(q, k_cache, v_cache, seq_lens, block_table, max_seq_len)
-    _check_weights(weights, q, k_cache)
-    _check_aux("alibi_slopes", alibi_slopes, torch.float32, (q.shape[1],), q.device)
     status, need, out, lse = _host().decode_weights(q, k_cache, v_cache, weights, seq_lens, block_table, max_seq_len,
                                                     *_paged_variant(q, scale, window, softcap, alibi_slopes), workspace, return_lse, _stream(q))
     if status:
@@ -520,10 +480,6 @@ def prefill_key_weights(q: torch.Tensor, k_cache: torch.Tensor, lse: torch.Tenso
     return_lse.  The newest Sq tokens' weights start at zero.  Returns `weights`.  Not differentiable."""
     if not q.is_cuda or q.dtype != torch.bfloat16 or q.dim() != 4:
         raise ValueError("prefill_key_weights() takes a bf16 CUDA q of shape [B, H, Sq, D]")
-    max_seq_len = _check_cache(q, k_cache, None, seq_lens, block_table, max_seq_len)
-    _check_weights(weights, q, k_cache)
-    _check_aux("lse", lse, torch.float32, tuple(q.shape[:3]), q.device, contiguous=False)
-    _check_aux("alibi_slopes", alibi_slopes, torch.float32, (q.shape[1],), q.device)
     status, need = _host().key_weights(q, k_cache, lse, weights, seq_lens, block_table, max_seq_len,
                                        *_paged_variant(q, scale, window, softcap, alibi_slopes), workspace, _stream(q))
     if status:
@@ -545,18 +501,8 @@ def evict_cache(weights: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Ten
     them).  Slots of different kv heads hold different tokens then, so that a window or ALiBi slopes no longer measure distances."""
     if not isinstance(weights, torch.Tensor) or not weights.is_cuda or weights.dim() != 3:
         raise ValueError("evict_cache() takes CUDA weights of shape [B, Hkv, capacity]")
-    max_seq_len = _check_cache(weights, k_cache, v_cache, seq_lens, block_table, max_seq_len)
-    _check_weights(weights, weights, k_cache)
-    if not isinstance(dst_table, torch.Tensor) or dst_table.dim() != 2:
-        raise ValueError("dst_table must be [B, pages]")
-    _check_aux("dst_table", dst_table, torch.int32, (weights.shape[0], dst_table.shape[1]), weights.device, contiguous=False, inner_unit=True)
-    if budget < 1 or dst_table.shape[1] * k_cache.shape[1] < budget:
-        raise ValueError(f"budget = {budget} with {dst_table.shape[1]} pages of {k_cache.shape[1]} tokens in dst_table")
-    capacity = budget if capacity is None else capacity
-    if capacity < budget:
-        raise ValueError(f"capacity = {capacity} is less than budget = {budget}")
-    status, new_lens, new_weights, kept = _host().evict(weights, k_cache, v_cache, seq_lens, block_table, dst_table, max_seq_len, int(budget),
-                                                        int(sinks), int(recent), int(capacity), _stream(weights))
+    status, new_lens, new_weights, kept = _host().evict(weights, k_cache, v_cache, seq_lens, block_table, dst_table, max_seq_len, budget, sinks,
+                                                        recent, capacity, _stream(weights))
     if status:
         fb.check(status)
     return new_lens, new_weights, kept
