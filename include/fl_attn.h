@@ -1,7 +1,8 @@
 /*
  * fl_attn.h -- C ABI of the fused attention-variant library for AMD MI355X (gfx950): the forward
  * pass of every variant, the backward pass of the variants without bias, gate and second stream, and the
- * decode step (one query per sequence over a paged key/value cache).
+ * decode step (one query per sequence over a paged key/value cache); and around that cache rotary positions, the
+ * weight that cached keys receive, and eviction by it.
  *
  * One call computes, for every (b, g, h) and every query row i, without ever writing the
  * [Sq, Sk] score matrix to device memory:
