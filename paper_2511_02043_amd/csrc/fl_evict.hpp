@@ -8,7 +8,10 @@
 //     and wait in LDS;
 //   * evict_move_kernel copies the rows that stay: no row has two readers or two writers, pages of the result are pages that nothing is
 //     read from, so the copy needs no order and runs over all of them at once.
-// Bound by the copy: 8 D bytes read and written per row and kv head beside the 4 bytes of a weight.
+// The copy moves 8 D bytes per row and kv head, beside the 4 bytes of a weight: at D = 128 64 sequences x 8 heads x 2048 rows in 220 us (4.9 TB/s, what a
+// large copy reaches), 8 x 8 x 2048 in 24.  The selection has a compute unit per (sequence, kv head): 12 us for 64 x 8 of 2049 - 2304 slots,
+// 28 for 8 x 8 of 16k - 32k, 7 for one short sequence, which is its chain of loads and barriers.  (Three copies of the first histogram, one per
+// lane modulo three, changed nothing: additions to one bin are not what holds it.)
 #pragma once
 #include "fl_params.hpp"
 
@@ -99,8 +102,15 @@ __global__ void __launch_bounds__(THREADS) evict_select_kernel(const EvictParams
     if (i < i0 + count) f(i, key_at(i));
   };
   if constexpr (HELD) {                            // (a thread reads back what it has written itself)
-#pragma unroll 8
-    for (int i = i0 + lane; i < i0 + count; i += 64) held[i] = weight_key(w[lo + i]);
+    constexpr int BATCH = THREADS == 256 ? 8 : 16;  // loads under way together: a trip to memory is longer than all the rest of a step
+    for (int at = 0; at < count; at += 64 * BATCH) {
+      float v[BATCH];
+#pragma unroll
+      for (int u = 0; u < BATCH; ++u) v[u] = at + 64 * u + lane < count ? w[lo + i0 + at + 64 * u + lane] : 0.f;
+#pragma unroll
+      for (int u = 0; u < BATCH; ++u)
+        if (at + 64 * u + lane < count) held[i0 + at + 64 * u + lane] = weight_key(v[u]);
+    }
   }
   for (int i = tid; i < 3 * kSelectBins / 4; i += THREADS) ((uint4*)&sh.hist[0][0])[i] = make_uint4(0, 0, 0, 0);
   __syncthreads();

@@ -6,6 +6,8 @@
 // pair: the work is memory traffic.  What could outgrow it is the angle: one sine and cosine per (token, pair), with the angle reduced in
 // 64 bits (a float's product with a position of 10^5 leaves 10^-2 of phase).  A thread therefore owns one token and VEC pairs, forms their
 // angles once and turns several heads with them; its pieces of a head are 16-byte loads and stores, neighbouring threads continue a row.
+// Measured: 2 x 8192 tokens, 32 / 8 heads, D = 128, bf16 80 us a pass (4.2 TB/s; a large copy 4.9), 8 x 512 tokens into the cache 19 - 22 (4.6 - 5.3), one
+// token of 64 sequences 5, a chain of loads: length, page, row.
 #pragma once
 #include "fl_params.hpp"
 

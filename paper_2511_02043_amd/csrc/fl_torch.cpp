@@ -246,7 +246,7 @@ std::tuple<int, int64_t, Tensor, OptTensor> paged(bool decode, const Tensor& q, 
 
 // ---- a bounded key/value cache: positions, weights of cached keys, eviction ----
 
-// The checks of these calls' tensors are here too: in Python they took 10 us of a 16 us call that turns one token of 64 sequences.
+// The checks of these calls' tensors are here too (one token of 64 sequences into the cache: 10.2 us a call with them in Python, 5.8 here).
 template <class... Parts>
 void need(bool ok, const Parts&... parts) {
   if (!ok) throw py::value_error(c10::str(parts...));
