@@ -580,14 +580,15 @@ std::tuple<int, Tensor> variant_node(const Tensor& q, const Tensor& k, const Ten
 struct Turned {
   const OptTensor &q, &k;
 };
+// Autograd keeps no tensors made in inference mode, which have no version to compare: a copy of one.
+Tensor savable(const Tensor& t) { return t.is_inference() ? t.clone() : t; }
 // The turn by -t of what arrives; itself differentiable, the map being linear.
 struct RotaryNode : torch::autograd::Function<RotaryNode> {
   static torch::autograd::variable_list forward(torch::autograd::AutogradContext* ctx, const OptTensor& q, const OptTensor&, const Tensor& positions,
                                                 const Tensor& inv_freq, const std::vector<int64_t>& sections, bool interleaved, bool inverse,
                                                 const Turned& turned) {
     ctx->set_materialize_grads(false);
-    ctx->saved_data["positions"] = positions;
-    ctx->saved_data["inv_freq"] = inv_freq;
+    ctx->save_for_backward({savable(positions), savable(inv_freq)});           // (changed in place before the backward pass: torch raises there)
     ctx->saved_data["sections"] = sections;
     ctx->saved_data["how"] = std::vector<int64_t>{q.has_value(), interleaved, inverse};
     torch::autograd::variable_list out;
@@ -598,7 +599,8 @@ struct RotaryNode : torch::autograd::Function<RotaryNode> {
   static torch::autograd::variable_list backward(torch::autograd::AutogradContext* ctx, const torch::autograd::variable_list& grads) {
     const auto how = ctx->saved_data["how"].toIntVector();
     const auto sections = ctx->saved_data["sections"].toIntVector();
-    const Tensor positions = ctx->saved_data["positions"].toTensor(), inv_freq = ctx->saved_data["inv_freq"].toTensor();
+    const auto saved = ctx->get_saved_variables();
+    const Tensor &positions = saved[0], &inv_freq = saved[1];
     const int first = how[0] != 0 ? 0 : 1;
     OptTensor g[2];                                // of q and k, where one has arrived and is wanted
     for (size_t n = 0; n < grads.size(); ++n)

@@ -383,15 +383,18 @@ class _Rotary(torch.autograd.Function):
 
     @staticmethod
     def forward(ctx, q, k, positions, inv_freq, sections, interleaved, inverse):
-        ctx.how, ctx.inverse = (positions, inv_freq, sections, interleaved), inverse
-        return _rotary_plain(q, k, ctx.how, inverse)
+        # changed in place before the backward pass, the saved ones raise there; autograd keeps no tensors made in inference mode: a copy
+        ctx.save_for_backward(*(t.clone() if t.is_inference() else t for t in (positions, inv_freq)))
+        ctx.how = sections, interleaved, inverse
+        return _rotary_plain(q, k, (positions, inv_freq, sections, interleaved), inverse)
 
     @staticmethod
     def backward(ctx, dq, dk):
         dq, dk = (_readable(g) if need else None for g, need in zip((dq, dk), ctx.needs_input_grad))
         if dq is None and dk is None:
             return (None,) * 7
-        return _Rotary.apply(dq, dk, *ctx.how, not ctx.inverse) + (None,) * 5
+        sections, interleaved, inverse = ctx.how
+        return _Rotary.apply(dq, dk, *ctx.saved_tensors, sections, interleaved, not inverse) + (None,) * 5
 
 
 def rotary(q: torch.Tensor, k: Optional[torch.Tensor], positions: torch.Tensor, inv_freq: torch.Tensor, *, sections=None,
@@ -402,9 +405,12 @@ def rotary(q: torch.Tensor, k: Optional[torch.Tensor], positions: torch.Tensor, 
     [B, S, axes] ([1, S, axes] for all sequences alike), up to four axes such as time, height and width; inv_freq float32 [pairs],
     2 * pairs <= D.  sections: the pairs of each axis, in order (None: one axis).  Pair i is the channels (i, i + pairs), or
     (2i, 2i + 1) with interleaved; channels from 2 * pairs on stay.  Returns the turned q and k, in their layouts; differentiable
-    (any number of times) in both."""
+    (any number of times) in both, not in inv_freq.  The backward pass reads positions and inv_freq again: changed in place before it, they
+    raise there."""
     if not q.is_cuda or q.dtype not in (torch.bfloat16, torch.float32) or q.dim() != 4:
         raise ValueError("rotary() takes a bf16 or float32 CUDA q of shape [B, H, S, D] (there is no CPU or fallback path)")
+    if getattr(inv_freq, "requires_grad", False) and _grad_enabled():
+        raise ValueError("inv_freq requires a gradient, and rotary() has none for it: pass inv_freq.detach()")
     sections = _tuple(sections)
     node = _node_for((q, k))
     if node == _PYTHON_NODE:
