@@ -365,8 +365,9 @@ fl_status fl_rotary_embed(const fl_tensor* q, const fl_tensor* k, const fl_rotar
  * (kv->seq_lens counts the new tokens already, as in the fl_attn_decode or fl_attn_prefill_paged call that follows).  Positions are the
  * caller's: a slot need not say where its token is in the sequence, so that a cache some tokens have been evicted from goes on as it is.
  *   q [B, 1, H, T, D], k and v [B, 1, Hkv, T, D]  bf16;  q_out as q (may be q itself);  rotary->inverse 0
- *   k_cache, v_cache, kv   as for fl_attn_decode, any D; written here.  Nothing is written for tokens at negative slots (len_b < T)
- *                          and for those whose table entry names no page of the cache. */
+ *   k_cache, v_cache, kv   as for fl_attn_decode, any D; written here.  Nothing is written for tokens at negative slots (len_b < T),
+ *                          for those at slots from kv->max_seq_len on (len_b above it is not cut here) and for those whose table entry names
+ *                          no page of the cache. */
 fl_status fl_rotary_append(const fl_tensor* q, const fl_tensor* k, const fl_tensor* v, const fl_rotary* rotary, const fl_paged_kv* kv,
                            fl_tensor* q_out, fl_tensor* k_cache, fl_tensor* v_cache, void* stream);
 

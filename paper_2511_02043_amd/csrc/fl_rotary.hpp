@@ -80,9 +80,9 @@ __global__ void __launch_bounds__(256) rotary_kernel(const RotaryParams p) {
   T* k_slot = nullptr;                             // APPEND: this token's row of kv head 0 in the caches; null: it has none
   T* v_slot = nullptr;
   if constexpr (APPEND) {
-    const int len = min(max(p.seq_lens[b], 0), p.max_len);
-    const int slot = len - p.S + s;
-    if (slot >= 0) {
+    // (from the true length: cut to the bound as in the calls that read, it would put the tokens on the slots of older ones)
+    const int slot = max(p.seq_lens[b], 0) - p.S + s;
+    if (slot >= 0 && slot < p.max_len) {
       int64_t page = b, in_page = slot;
       if (p.block_table != nullptr) {
         page = p.block_table[(int64_t)b * p.table_stride + (slot >> p.page_shift)];

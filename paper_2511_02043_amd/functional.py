@@ -436,7 +436,8 @@ def rotary_append(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, positions: 
 
     q [B, H, T, D] with k, v [B, Hkv, T, D], or without the T axis for one token; bf16.  positions int32 [B, T, axes]: where the tokens
     are in their sequences, which after an eviction is not their slot.  Caches, seq_lens, block_table, max_seq_len as for
-    decode_attention(); tokens at negative slots and table entries that name no page are passed over.  Not differentiable."""
+    decode_attention(); tokens at negative slots and at slots from max_seq_len on, and table entries that name no page, are passed over.
+    Not differentiable."""
     if not q.is_cuda or q.dtype != torch.bfloat16 or q.dim() not in (3, 4):
         raise ValueError("rotary_append() takes a bf16 CUDA q of shape [B, H, T, D] or [B, H, D]")
     status, out = _host().rotary_append(q, k, v, positions, inv_freq, _tuple(sections), bool(interleaved), k_cache, v_cache, seq_lens, block_table,
