@@ -347,7 +347,25 @@ fl_status fl_cache_evict(const fl_tensor* weights, fl_tensor* k_cache, fl_tensor
     return fail(FL_ERR_SHAPE, "dst_stride %d is less than the pages of budget", evict->dst_stride);
   if ((st = check_weights(weights, "weights", B, Hkv, kv->max_seq_len)) != FL_OK) return st;
   if ((st = check_weights(new_weights, "new_weights", B, Hkv, evict->budget)) != FL_OK) return st;
-  if (weights->ptr == new_weights->ptr) return fail(FL_ERR_DESC, "new_weights is weights");
+  // workgroups read lengths, tables and weights while others write: no output may share memory with those or with another
+  {
+    using fl::host::Rows;
+    const int64_t src_pages = (kv->max_seq_len + page_size - 1) / page_size, dst_pages = (evict->budget + page_size - 1) / page_size;
+    auto of = [&](const fl_tensor* t, int64_t n) {
+      return Rows{(uintptr_t)t->ptr, B, B > 1 ? t->stride[0] * 4 : 0, Hkv, Hkv > 1 ? t->stride[2] * 4 : 0, n * 4};
+    };
+    const struct { const char* name; Rows rows; } all[] = {
+        {"new_lens", fl::host::flat_rows(evict->new_lens, B * 4)},
+        {"kept", fl::host::flat_rows(evict->kept, B * Hkv * evict->budget * 4)},
+        {"new_weights", of(new_weights, new_weights->size[4])},
+        {"seq_lens", fl::host::flat_rows(kv->seq_lens, B * 4)},
+        {"dst_table", Rows{(uintptr_t)evict->dst_table, B, evict->dst_stride * 4LL, 1, 0, dst_pages * 4}},
+        {"block_table", Rows{(uintptr_t)kv->block_table, kv->block_table != nullptr ? B : 0, kv->table_stride * 4LL, 1, 0, src_pages * 4}},
+        {"weights", of(weights, kv->max_seq_len)}};
+    for (int o = 0; o < 3; ++o)
+      for (int i = o + 1; i < 7; ++i)
+        if (rows_meet(all[o].rows, all[i].rows)) return fail(FL_ERR_DESC, "%s and %s share memory", all[o].name, all[i].name);
+  }
   if (B * Hkv > 0x7fffffffLL) return fail(FL_ERR_SHAPE, "too many workgroups");
 
   fl::EvictParams p;

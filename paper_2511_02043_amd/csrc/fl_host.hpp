@@ -93,6 +93,49 @@ inline fl::View make_view(const fl_tensor* t) {
   return v;
 }
 
+// Rows of `bytes` each in memory: n0 x n1 of them, s0 and s1 bytes apart (>= bytes where there are several).
+struct Rows {
+  uintptr_t at;
+  int64_t n0, s0, n1, s1, bytes;
+};
+inline Rows flat_rows(const void* p, int64_t bytes) { return {(uintptr_t)p, 1, 0, 1, 0, bytes}; }
+// The first byte behind them; -1 where that is past every address.
+inline int64_t rows_end(const Rows& r) {
+  const __int128 e = (__int128)r.at + (__int128)(r.n0 - 1) * r.s0 + (__int128)(r.n1 - 1) * r.s1 + r.bytes;
+  return e > (__int128)INT64_MAX ? -1 : (int64_t)e;
+}
+// True where `la` bytes from x on and rows of `lb` bytes at 0, s, 2 s, ... (n of them, s >= lb) have a byte in common.
+inline bool row_meets(int64_t x, int64_t la, int64_t n, int64_t s, int64_t lb) {
+  if (n == 1 || x < 0) return x < lb && x + la > 0;        // (from before the first row: that one or none)
+  const int64_t i = x / s < n - 1 ? x / s : n - 1;         // the last row that starts at x or before
+  return x < i * s + lb || (i + 1 < n && x + la > (i + 1) * s);
+}
+// True where a row of `a` and a row of `b` have a byte in common: exactly, since two views may take turns in one buffer.
+inline bool rows_meet(const Rows& a, Rows b) {
+  if (a.n0 <= 0 || a.n1 <= 0 || a.bytes <= 0 || b.n0 <= 0 || b.n1 <= 0 || b.bytes <= 0) return false;
+  const int64_t end_a = rows_end(a), end_b = rows_end(b);
+  if (end_a < 0 || end_b < 0) return true;                 // (no memory is like that)
+  if (end_a <= (int64_t)b.at || end_b <= (int64_t)a.at) return false;
+  if (b.n0 == 1 || (b.n1 > 1 && b.s1 > b.s0)) {            // axis 0 the one of the larger steps
+    int64_t t = b.n0;
+    b.n0 = b.n1, b.n1 = t;
+    t = b.s0;
+    b.s0 = b.s1, b.s1 = t;
+  }
+  const bool nested = b.n0 == 1 || (b.n1 - 1) * b.s1 + b.bytes <= b.s0;
+  for (int64_t i0 = 0; i0 < a.n0; ++i0)
+    for (int64_t i1 = 0; i1 < a.n1; ++i1) {
+      const int64_t x = (int64_t)a.at + i0 * a.s0 + i1 * a.s1 - (int64_t)b.at;
+      // of b's groups of rows, where they follow each other: the last one that starts at x or before, and the next (a row that reaches past
+      // that one's start meets its first row)
+      const int64_t j = !nested || b.n0 == 1 || x < 0 ? 0 : (x / b.s0 < b.n0 - 1 ? x / b.s0 : b.n0 - 1);
+      const int64_t j_end = nested && j + 2 < b.n0 ? j + 2 : b.n0;
+      for (int64_t j0 = j; j0 < j_end; ++j0)
+        if (row_meets(x - j0 * b.s0, a.bytes, b.n1, b.s1, b.bytes)) return true;
+    }
+  return false;
+}
+
 // The accumulated weights of cached keys, [B, 1, Hkv, 1, C] f32 with C >= least.
 inline fl_status check_weights(const fl_tensor* t, const char* name, int64_t B, int64_t Hkv, int64_t least) {
   if (t == nullptr || t->ptr == nullptr) return fail(FL_ERR_NULL, "%s is NULL", name);
