@@ -139,6 +139,7 @@ fl_status fl_rotary_append(const fl_tensor* q, const fl_tensor* k, const fl_tens
   int page_shift = 0;
   if ((st = check_cache(kv, k_cache, v_cache, B, Hkv, D, &page_shift)) != FL_OK) return st;
   if (B * T == 0) return FL_OK;
+  if (kv->seq_lens == nullptr) return fail(FL_ERR_NULL, "seq_lens is NULL");   // (queries alone, which the check of the cache lets pass, read it too)
   const int64_t qs[5] = {B, 1, H, T, D}, ks[5] = {B, 1, Hkv, T, D};
   if (H > 0) {
     if ((st = check_data_tensor(q, "q", FL_BF16, qs)) != FL_OK || (st = check_data_tensor(q_out, "q_out", FL_BF16, qs)) != FL_OK) return st;
