@@ -208,6 +208,17 @@ std::tuple<int, std::vector<OptTensor>> variant_bwd(const Tensor& q, const Tenso
   return {status, {dq, dk, dv, dq2, dk2, dlam, dgate, dbias0, dbias1, drms}};
 }
 
+template <class... Parts>
+void need(bool ok, const Parts&... parts) {
+  if (!ok) throw py::value_error(c10::str(parts...));
+}
+// A caller's workspace is written through its address alone, nbytes() of it from there on: memory of the call's device without gaps or repeats.
+void check_workspace(const OptTensor& workspace, const Tensor& q) {
+  need(!workspace.has_value() || workspace->device() == q.device(), "workspace must be on ", q.device());
+  need(!workspace.has_value() || workspace->is_non_overlapping_and_dense(), "workspace must be contiguous memory, got strides ",
+       workspace.has_value() ? workspace->strides() : at::IntArrayRef());
+}
+
 // A decode step (q [B, H, D]) or a chunk of a paged prefill (q [B, H, Sq, D]) over caches [pages, page_size, Hkv, D].  Returns
 // the status, the workspace bytes the call needs, out (q's shape) and lse ([B, H] or [B, H, Sq]; undefined unless wanted).  A
 // workspace that is too small is reported by the second value alone: nothing has been launched then.
@@ -216,6 +227,7 @@ std::tuple<int, int64_t, Tensor, OptTensor> paged(bool decode, const Tensor& q, 
                                                   int mod, double softcap, int mask, int window, const OptTensor& slopes,
                                                   const OptTensor& workspace, bool want_lse, int64_t stream) {
   TORCH_CHECK(k_cache.dim() == 4 && v_cache.dim() == 4, "the caches must be [pages, page_size, Hkv, D]");
+  check_workspace(workspace, q);
   const fl_tensor tq = decode ? desc5(q, {0, -1, 1, -1, 2}) : desc5(q, {0, -1, 1, 2, 3});
   const fl_tensor tk = desc5(k_cache, {0, -1, 2, 1, 3}), tv = desc5(v_cache, {0, -1, 2, 1, 3});
   Tensor out = at::empty(q.sizes(), q.options());
@@ -247,10 +259,6 @@ std::tuple<int, int64_t, Tensor, OptTensor> paged(bool decode, const Tensor& q, 
 // ---- a bounded key/value cache: positions, weights of cached keys, eviction ----
 
 // The checks of these calls' tensors are here too (one token of 64 sequences into the cache: 10.2 us a call with them in Python, 5.8 here).
-template <class... Parts>
-void need(bool ok, const Parts&... parts) {
-  if (!ok) throw py::value_error(c10::str(parts...));
-}
 // an array that the C ABI reads as raw memory of a fixed type and shape
 void check_array(const char* name, const OptTensor& t, at::ScalarType dtype, at::IntArrayRef shape, at::Device device, bool contiguous, bool inner_unit) {
   need(t.has_value(), name, " must be a torch.Tensor");
@@ -397,6 +405,7 @@ std::tuple<int, int64_t, Tensor, OptTensor> decode_weights(const Tensor& q, cons
   const int max_seq_len = (int)check_cache(q, k_cache, v_cache, lens, table, bound);
   check_weights(w, q, k_cache);
   check_slopes(slopes, q);
+  check_workspace(workspace, q);
   const Tensor &weights = *w, &seq_lens = *lens;
   const fl_tensor tq = rows_desc(q), tk = cache_desc(k_cache), tv = cache_desc(v_cache);
   Tensor out = at::empty(q.sizes(), q.options());
@@ -425,6 +434,7 @@ std::tuple<int, int64_t> key_weights(const Tensor& q, const Tensor& k_cache, con
   check_weights(w, q, k_cache);
   check_array("lse", lse, at::kFloat, {q.size(0), q.size(1), q.size(2)}, q.device(), false, false);
   check_slopes(slopes, q);
+  check_workspace(workspace, q);
   const Tensor &weights = *w, &seq_lens = *lens;
   const fl_tensor tq = rows_desc(q), tk = cache_desc(k_cache), tlse = desc5(*lse, {0, -1, 1, 2, -1});
   fl_tensor tw = desc5(weights, {0, -1, 1, -1, 2});
