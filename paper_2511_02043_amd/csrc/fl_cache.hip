@@ -346,7 +346,7 @@ fl_status fl_cache_evict(const fl_tensor* weights, fl_tensor* k_cache, fl_tensor
   if (evict->new_lens == nullptr || evict->kept == nullptr || evict->dst_table == nullptr) return fail(FL_ERR_NULL, "new_lens, kept or dst_table is NULL");
   if (evict->dst_stride < ((int64_t)evict->budget + page_size - 1) / page_size)
     return fail(FL_ERR_SHAPE, "dst_stride %d is less than the pages of budget", evict->dst_stride);
-  if ((st = check_weights(weights, "weights", B, Hkv, kv->max_seq_len)) != FL_OK) return st;
+  if ((st = check_weights(weights, "weights", B, Hkv, kv->max_seq_len, false)) != FL_OK) return st;
   if ((st = check_weights(new_weights, "new_weights", B, Hkv, evict->budget)) != FL_OK) return st;
   // workgroups read lengths, tables and weights while others write: no output may share memory with those or with another
   {

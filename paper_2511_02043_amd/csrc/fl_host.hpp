@@ -136,8 +136,20 @@ inline bool rows_meet(const Rows& a, Rows b) {
   return false;
 }
 
-// The accumulated weights of cached keys, [B, 1, Hkv, 1, C] f32 with C >= least.
-inline fl_status check_weights(const fl_tensor* t, const char* name, int64_t B, int64_t Hkv, int64_t least) {
+// True where two rows of n0 x n1, s0 and s1 elements apart, `len` long (<= each step where there are several), lie over each other.
+inline bool rows_overlap(int64_t n0, int64_t s0, int64_t n1, int64_t s1, int64_t len) {
+  if (n0 <= 1 || n1 <= 1) return false;
+  typedef __int128 wide;
+  if ((wide)(n1 - 1) * s1 + len <= s0 || (wide)(n0 - 1) * s0 + len <= s1) return false;   // one axis within a step of the other
+  for (int64_t i = 1; i < n0; ++i) {               // rows i apart along the first axis: the nearest ones along the second, on either side
+    const wide k = (wide)i * s0 / s1, rest = (wide)i * s0 % s1;
+    if ((k < n1 && rest < len) || (k + 1 < n1 && s1 - rest < len)) return true;
+  }
+  return false;
+}
+
+// The accumulated weights of cached keys, [B, 1, Hkv, 1, C] f32 with C >= least.  `written`: each row by a workgroup of its own.
+inline fl_status check_weights(const fl_tensor* t, const char* name, int64_t B, int64_t Hkv, int64_t least, bool written = true) {
   if (t == nullptr || t->ptr == nullptr) return fail(FL_ERR_NULL, "%s is NULL", name);
   if (t->dtype != FL_F32) return fail(FL_ERR_DTYPE, "%s must be f32", name);
   const int64_t want[4] = {B, 1, Hkv, 1};
@@ -151,6 +163,8 @@ inline fl_status check_weights(const fl_tensor* t, const char* name, int64_t B, 
   if (((uintptr_t)t->ptr) % 4 != 0) return fail(FL_ERR_ALIGN, "%s base pointer not 4-byte aligned", name);
   for (int a = 0; a < 4; a += 2)
     if (t->size[a] > 1 && t->stride[a] < t->size[4]) return fail(FL_ERR_STRIDE, "%s stride[%d]: rows overlap", name, a);
+  if (written && rows_overlap(B, t->stride[0], Hkv, t->stride[2], t->size[4]))
+    return fail(FL_ERR_STRIDE, "%s strides %lld and %lld: rows overlap", name, (long long)t->stride[0], (long long)t->stride[2]);
   return FL_OK;
 }
 
