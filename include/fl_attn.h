@@ -422,8 +422,9 @@ typedef struct {
  *   weights       [B, 1, Hkv, 1, C] f32, C >= kv->max_seq_len, as the calls above have left them
  *   k_cache, v_cache, kv   as for fl_attn_decode (any D, bf16); with a page size that is a power of two >= 8, also without a block table
  *   new_weights   [B, 1, Hkv, 1, C2] f32, C2 >= budget, unit inner stride: the weights of what stays, zero from new_lens[b] to C2
- * Nothing is copied to a destination whose table entry names no page of the cache.  new_lens, kept and new_weights share no memory with one
- * another nor with seq_lens, the tables and weights (FL_ERR_DESC): other workgroups may still have these to read. */
+ * Nothing is copied to a destination whose table entry names no page of the cache, and zeros from a source whose entry does not.
+ * new_lens, kept and new_weights share no memory with one another nor with seq_lens, the tables and weights (FL_ERR_DESC): other
+ * workgroups may still have these to read. */
 fl_status fl_cache_evict(const fl_tensor* weights, fl_tensor* k_cache, fl_tensor* v_cache, const fl_paged_kv* kv, const fl_evict* evict,
                          fl_tensor* new_weights, void* stream);
 

@@ -210,13 +210,16 @@ __global__ void __launch_bounds__(256) evict_move_kernel(const EvictParams p) {
     const int j = kept[r];
     int64_t page = b, off = j;
     if (p.block_table != nullptr) {
-      page = min(max(p.block_table[(int64_t)b * p.table_stride + (j >> p.page_shift)], 0), p.num_pages - 1);
+      page = p.block_table[(int64_t)b * p.table_stride + (j >> p.page_shift)];
       off = j & in_page;
     }
     const int to = p.dst_table[(int64_t)b * p.dst_stride + (r >> p.page_shift)];
     if (to < 0 || to >= p.num_pages) continue;
-    const uint4 x = *(const uint4*)(p.k_cache + page * p.k_sp + off * p.k_st + h * p.k_sh + piece * 8);
-    const uint4 y = *(const uint4*)(p.v_cache + page * p.v_sp + off * p.v_st + h * p.v_sh + piece * 8);
+    uint4 x = make_uint4(0, 0, 0, 0), y = x;       // a token whose entry names no page has no row: not one of another page's
+    if (page >= 0 && page < p.num_pages) {
+      x = *(const uint4*)(p.k_cache + page * p.k_sp + off * p.k_st + h * p.k_sh + piece * 8);
+      y = *(const uint4*)(p.v_cache + page * p.v_sp + off * p.v_st + h * p.v_sh + piece * 8);
+    }
     *(uint4*)(p.k_cache + (int64_t)to * p.k_sp + (int64_t)(r & in_page) * p.k_st + h * p.k_sh + piece * 8) = x;
     *(uint4*)(p.v_cache + (int64_t)to * p.v_sp + (int64_t)(r & in_page) * p.v_st + h * p.v_sh + piece * 8) = y;
   }

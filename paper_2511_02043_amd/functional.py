@@ -503,9 +503,10 @@ def evict_cache(weights: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Ten
 
     weights float32 [B, Hkv, >= max_seq_len]; caches bf16, lengths and block_table as for decode_attention(); dst_table int32
     [B, >= budget / page_size]: pages of the same caches that no sequence of the call is read from.  Afterwards a sequence lives in its
-    dst_table pages, and its old ones are the caller's to hand out again.  Returns the new lengths int32 [B], the weights of what stays float32
-    [B, Hkv, capacity] (zero behind them; capacity >= budget, by default budget), and the kept slots int32 [B, Hkv, budget] (-1 behind
-    them).  Slots of different kv heads hold different tokens then, so that a window or ALiBi slopes no longer measure distances."""
+    dst_table pages, and its old ones are the caller's to hand out again.  A token whose entry in block_table names no page has zeros in its
+    place.  Returns the new lengths int32 [B], the weights of what stays float32 [B, Hkv, capacity] (zero behind them; capacity >= budget, by
+    default budget), and the kept slots int32 [B, Hkv, budget] (-1 behind them).  Slots of different kv heads hold different tokens then, so
+    that a window or ALiBi slopes no longer measure distances."""
     if not isinstance(weights, torch.Tensor) or not weights.is_cuda or weights.dim() != 3:
         raise ValueError("evict_cache() takes CUDA weights of shape [B, Hkv, capacity]")
     status, new_lens, new_weights, kept = _host().evict(weights, k_cache, v_cache, seq_lens, block_table, dst_table, max_seq_len, budget, sinks,
