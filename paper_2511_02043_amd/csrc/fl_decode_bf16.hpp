@@ -509,14 +509,17 @@ __global__ void __launch_bounds__(64) decode_finish_kernel(const DecodeParams p)
     const float of_lane = __shfl(mine, ((lane - c0) & (per - 1)) * span);
     if (lane >= c0 && lane < c0 + per) lse2 = of_lane;
   }
+  const uint32_t reach = (uint32_t)(p.window >= 0 ? p.window : p.max_len);   // how far behind a row its keys go
   float gained[KPL] = {};
   for (int c0 = 0; c0 < ncol; c0 += CU) {
     if (c0 > 0) load(c0);
 #pragma unroll
     for (int c = 0; c < CU; ++c) {
       const float ref = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(lse2), min(c0 + c, ncol - 1)));
+      // what a row's mask hides is told by its position: -inf less the NaN of a row that sees one would be NaN
+      const int pos = len - p.T + p.by_group.div(c0 + c);
 #pragma unroll
-      for (int i = 0; i < KPL; ++i) gained[i] += c0 + c < ncol && scored[i] ? fast_exp2(x[c][i] - ref) : 0.f;
+      for (int i = 0; i < KPL; ++i) gained[i] += c0 + c < ncol && (uint32_t)(pos - j[i]) <= reach ? fast_exp2(x[c][i] - ref) : 0.f;
     }
   }
 #pragma unroll
