@@ -509,19 +509,27 @@ __global__ void __launch_bounds__(64) decode_finish_kernel(const DecodeParams p)
     const float of_lane = __shfl(mine, ((lane - c0) & (per - 1)) * span);
     if (lane >= c0 && lane < c0 + per) lse2 = of_lane;
   }
-  const uint32_t reach = (uint32_t)(p.window >= 0 ? p.window : p.max_len);   // how far behind a row its keys go
   float gained[KPL] = {};
-  for (int c0 = 0; c0 < ncol; c0 += CU) {
-    if (c0 > 0) load(c0);
+  auto add = [&](auto by_position) __attribute__((always_inline)) {
+    const uint32_t reach = (uint32_t)(p.window >= 0 ? p.window : p.max_len);   // how far behind a row its keys go
+    for (int c0 = 0; c0 < ncol; c0 += CU) {
+      if (c0 > 0) load(c0);
 #pragma unroll
-    for (int c = 0; c < CU; ++c) {
-      const float ref = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(lse2), min(c0 + c, ncol - 1)));
-      // what a row's mask hides is told by its position: -inf less the NaN of a row that sees one would be NaN
-      const int pos = len - p.T + p.by_group.div(c0 + c);
+      for (int c = 0; c < CU; ++c) {
+        const float ref = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(lse2), min(c0 + c, ncol - 1)));
+        const int pos = len - p.T + p.by_group.div(c0 + c);
 #pragma unroll
-      for (int i = 0; i < KPL; ++i) gained[i] += c0 + c < ncol && (uint32_t)(pos - j[i]) <= reach ? fast_exp2(x[c][i] - ref) : 0.f;
+        for (int i = 0; i < KPL; ++i) {
+          const bool adds = decltype(by_position)::value ? (uint32_t)(pos - j[i]) <= reach : scored[i];
+          gained[i] += c0 + c < ncol && adds ? fast_exp2(x[c][i] - ref) : 0.f;
+        }
+      }
     }
-  }
+  };
+  // A hidden score is -inf, which tells all that is needed but for a row whose lse is NaN: -inf less NaN would be NaN.  (By position alone the
+  // step of 16 x 4 rows on 2k - 4k tokens, 32 / 8 heads, D = 128, took 66.8 instead of 65.5 us.)
+  if (__builtin_amdgcn_ballot_w64(lse2 != lse2) == 0) add(std::integral_constant<bool, false>{});
+  else add(std::integral_constant<bool, true>{});
 #pragma unroll
   for (int i = 0; i < KPL; ++i)
     if (j[i] < len) w[j[i]] = old[i] + gained[i];
