@@ -51,6 +51,14 @@ struct KeyWeightCfg : BwdCfg<D_, MOD_, 0, 64, 2> {
   static constexpr int IPW = (Base::TILE_INSTR + NW - 1) / NW;           // row loads of a wave per stage; wave 0 loads the lse, too
 };
 
+// A capped score cap tanh(s / cap) is s tanh(z) / z with z = s / cap, and tanh(z) / z the cubic 1 + c1 z^2 + c2 z^4 + c3 z^6 to 2^-28 while z is
+// below kCapNear (fitted to the largest error up to there).  Beyond, cap - 2 cap / (exp(2 z) + 1): it subtracts numbers of the cap's size, so
+// that its roundings are those of scores four times as large; scores of up to 6 under a cap of 1000 would lose 10^-4 of their probabilities.  Up to a
+// cap of kCapFar those roundings are below 2^-20 for any score, and no block is asked.  (8 chunks of 512 rows on 4k - 8k keys, 32 / 8 heads, us: cap 30,
+// D = 128 and 64, 362 and 289, with the quotient everywhere 387 and 338; cap 12, where most blocks have a score beyond, 404 and 386; cap 5 397, and
+// 404 with blocks asked.)
+constexpr float kCapNear = 0.25f, kCapFar = 8.f, kCap1 = -0.33333242f, kCap2 = 0.13324264f, kCap3 = -0.05143305f;
+
 template <class C>
 __global__ void __launch_bounds__(C::NW * 64) __attribute__((amdgpu_waves_per_eu(4, 4))) key_weights_kernel(const KeyWeightParams p) {
   constexpr int D = C::D, KK = C::KK, ROW = C::ROW;
@@ -98,6 +106,21 @@ __global__ void __launch_bounds__(C::NW * 64) __attribute__((amdgpu_waves_per_eu
     for (int kk = 0; kk < KK; ++kk) kf[kk] = *(const bf16x8*)(row + 16 * kk + 8 * w.half);
   }
   const float c_scale = p.scale * kLog2e;
+  // soft-cap: where all raw scores of a block are below near_to, s * (near0 + near1 s^2 + ...) scales and caps them at once; exp2(s * far_in) is
+  // exp(2 z), cap_l2 the cap in the log2 domain.  (Within the bounds both and twice them are finite; beyond them a cap changes nothing, or all scores
+  // are 0.  near_to keeps the powers finite.)
+  float cap_l2 = 0.f, far_in = 0.f, near_to = 0.f, near0 = 0.f, near1 = 0.f, near2 = 0.f, near3 = 0.f;
+  if constexpr (C::MOD == kModSoftcap) {
+    auto uniform = [](float x) { return __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(x))); };
+    const float cap = fminf(fmaxf(p.softcap, 0x1p-120f), 0x1p120f), z1 = p.scale / cap, square = z1 * z1;   // z of a raw score of 1
+    cap_l2 = uniform(cap * kLog2e);
+    far_in = uniform(2.f * c_scale / cap);
+    near0 = uniform(c_scale);
+    near1 = uniform(c_scale * kCap1 * square);
+    near2 = uniform(c_scale * kCap2 * square * square);
+    near3 = uniform(c_scale * kCap3 * square * square * square);
+    near_to = cap > kCapFar && fabsf(near3) < 0x1p100f ? uniform(fminf(kCapNear / z1, 0x1p60f)) : 0.f;
+  }
 
   int ld_head = 0, ld_tile = 0;                    // next item to request
   // byte offsets of this lane's pieces in a whole tile: rows are below 2^23 elements apart, so 32 bits hold them
@@ -182,18 +205,27 @@ __global__ void __launch_bounds__(C::NW * 64) __attribute__((amdgpu_waves_per_eu
       // row and key `gap` apart, register by register: visible from 0 to `reach` (keys past the length may hold anything)
       const int gap = p_lo + 4 * w.half - j;
       float x[16];
+      if constexpr (C::MOD == kModSoftcap) {
+        float largest = INFINITY;
+        if (near_to > 0.f) {
+          largest = 0.f;                           // (NaN is left out: it comes out as NaN either way)
 #pragma unroll
-      for (int r = 0; r < 16; ++r) {
-        float a;
-        if constexpr (C::MOD == kModSoftcap) {
-          const float e = fast_exp2(s[r] * (2.f * c_scale / p.softcap));
-          a = fmaf(fast_rcp(e + 1.f), -2.f * p.softcap * kLog2e, p.softcap * kLog2e) + nl[r];
-        } else if constexpr (C::MOD == kModAlibi) {
-          a = fmaf(s[r], c_scale, fmaf(-slope2, (float)(gap + 8 * (r >> 2) + (r & 3)), nl[r]));
-        } else {
-          a = fmaf(s[r], c_scale, nl[r]);
+          for (int r = 0; r < 16; ++r) largest = fmaxf(largest, fabsf(s[r]));
         }
-        x[r] = fast_exp2(a);
+        if (__builtin_amdgcn_ballot_w64(largest >= near_to) == 0) {
+#pragma unroll
+          for (int r = 0; r < 16; ++r) {
+            const float y = s[r] * s[r];
+            x[r] = fast_exp2(fmaf(s[r], fmaf(y, fmaf(y, fmaf(y, near3, near2), near1), near0), nl[r]));
+          }
+        } else {
+#pragma unroll
+          for (int r = 0; r < 16; ++r) x[r] = fast_exp2(fmaf(__int_as_float(ls[r >> 2][r & 3]), -kLog2e, fmaf(fast_rcp(fast_exp2(s[r] * far_in) + 1.f), -2.f * cap_l2, cap_l2)));
+        }
+      } else {
+#pragma unroll
+        for (int r = 0; r < 16; ++r)
+          x[r] = fast_exp2(fmaf(s[r], c_scale, C::MOD == kModAlibi ? fmaf(-slope2, (float)(gap + 8 * (r >> 2) + (r & 3)), nl[r]) : nl[r]));
       }
       if (partial) {
 #pragma unroll
