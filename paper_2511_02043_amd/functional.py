@@ -379,22 +379,30 @@ def _readable(t):
 
 
 class _Rotary(torch.autograd.Function):
-    """rotary() where transforms, traces or torch.compile look into the node; the turn back is the same node."""
+    """rotary() where torch.func's grad, traces or torch.compile look into the node; the turn back is the same node.  (It has no rule for vmap and
+    none for forward-mode derivatives: torch refuses both.)"""
 
     @staticmethod
-    def forward(ctx, q, k, positions, inv_freq, sections, interleaved, inverse):
-        # changed in place before the backward pass, the saved ones raise there; autograd keeps no tensors made in inference mode: a copy
-        ctx.save_for_backward(*(t.clone() if t.is_inference() else t for t in (positions, inv_freq)))
-        ctx.how = sections, interleaved, inverse
+    def forward(q, k, positions, inv_freq, sections, interleaved, inverse, arrived=False):
+        if arrived:                                # gradients, in any layout; here they have addresses, in backward() under a transform not
+            q, k = _readable(q), _readable(k)
         return _rotary_plain(q, k, (positions, inv_freq, sections, interleaved), inverse)
 
     @staticmethod
+    def setup_context(ctx, inputs, output):
+        _, _, positions, inv_freq, *how = inputs
+        ctx.how = tuple(how[:3])
+        # changed in place before the backward pass, the saved ones raise there; autograd keeps no tensors made in inference mode: a copy
+        ctx.save_for_backward(*(t.clone() if t.is_inference() else t for t in (positions, inv_freq)))
+
+    @staticmethod
     def backward(ctx, dq, dk):
-        dq, dk = (_readable(g) if need else None for g, need in zip((dq, dk), ctx.needs_input_grad))
+        dq, dk = (g if need else None for g, need in zip((dq, dk), ctx.needs_input_grad))
+        rest = (None,) * (len(ctx.needs_input_grad) - 2)
         if dq is None and dk is None:
-            return (None,) * 7
+            return (None, None) + rest
         sections, interleaved, inverse = ctx.how
-        return _Rotary.apply(dq, dk, *ctx.saved_tensors, sections, interleaved, not inverse) + (None,) * 5
+        return _Rotary.apply(dq, dk, *ctx.saved_tensors, sections, interleaved, not inverse, True) + rest
 
 
 def rotary(q: torch.Tensor, k: Optional[torch.Tensor], positions: torch.Tensor, inv_freq: torch.Tensor, *, sections=None,

@@ -40,3 +40,26 @@ def test_positions_made_in_inference_mode():
         pos, inv = torch.full((1, 4, 1), 3, dtype=torch.int32), torch.ones(8)
     F._Rotary.apply(q, None, pos, inv, (8,), False, False)[0].sum().backward()
     assert torch.equal(q.grad, torch.full_like(q, -3.0))
+
+
+def test_func_grad_looks_into_the_node():
+    pos, inv = torch.arange(1, 5, dtype=torch.int32).reshape(1, 4, 1), torch.ones(8)
+    f = pos.reshape(1, 1, 4, 1).float()
+    cube = lambda q: (F._Rotary.apply(q, None, pos, inv, (8,), False, False)[0] ** 3).sum()
+    both = lambda q, k: sum((x ** 3).sum() for x in F._Rotary.apply(q, k, pos, inv, (8,), False, False))
+    torch.manual_seed(0)
+    q, k = torch.randn(1, 2, 4, 16), torch.randn(1, 1, 4, 16)
+    # y = f q, and the stand-in's turn back is -f
+    assert torch.allclose(torch.func.grad(cube)(q), -3 * f ** 3 * q ** 2)
+    for got, x in zip(torch.func.grad(both, argnums=(0, 1))(q, k), (q, k)):
+        assert torch.allclose(got, -3 * f ** 3 * x ** 2)
+    twice = torch.func.grad(lambda x: torch.func.grad(cube)(x).sum())(q)
+    # back through the turn back (a turn, f), the square's 6 y, and the first turn (-f)
+    assert torch.allclose(twice, -6 * f ** 3 * q)
+
+
+@pytest.mark.parametrize("transform", [lambda f, q: torch.func.vmap(f)(q[None]), lambda f, q: torch.func.jvp(f, (q,), (q,))])
+def test_transforms_without_a_rule_are_refused(transform):
+    pos, inv = torch.ones(1, 4, 1, dtype=torch.int32), torch.ones(8)
+    with pytest.raises(RuntimeError):
+        transform(lambda q: F._Rotary.apply(q, None, pos, inv, (8,), False, False)[0], torch.ones(1, 2, 4, 16))
