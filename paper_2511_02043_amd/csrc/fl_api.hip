@@ -2390,7 +2390,7 @@ static fl_status decode_call(const fl_tensor* q, const fl_tensor* k_cache, const
   p.num_pages = (int)pages;
   p.window = (mask & FL_MASK_WINDOW) ? clamp_window(desc->window, kv->max_seq_len, kv->max_seq_len) : -1;
   p.scale = desc->scale;
-  p.softcap = desc->softcap;
+  p.softcap = std::fmin(std::fmax(desc->softcap, 0x1p-120f), 0x1p120f);   // (both and twice them finite; beyond them every score is 0 in fp32, as at them)
   hipStream_t stream = (hipStream_t)stream_v;
   if (weights != nullptr) {
     p.weights = (float*)weights->ptr;
