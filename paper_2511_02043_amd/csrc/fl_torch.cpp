@@ -219,6 +219,9 @@ void check_workspace(const OptTensor& workspace, const Tensor& q) {
        workspace.has_value() ? workspace->strides() : at::IntArrayRef());
 }
 
+// From row to row of a table; a single row's stride says nothing.
+int32_t row_step(const Tensor& table) { return (int32_t)(table.size(0) > 1 ? table.stride(0) : table.size(1)); }
+
 // A decode step (q [B, H, D]) or a chunk of a paged prefill (q [B, H, Sq, D]) over caches [pages, page_size, Hkv, D].  Returns
 // the status, the workspace bytes the call needs, out (q's shape) and lse ([B, H] or [B, H, Sq]; undefined unless wanted).  A
 // workspace that is too small is reported by the second value alone: nothing has been launched then.
@@ -241,7 +244,7 @@ std::tuple<int, int64_t, Tensor, OptTensor> paged(bool decode, const Tensor& q, 
   fl_paged_kv kv = {};
   kv.struct_size = sizeof(kv);
   kv.block_table = ptr<const int32_t>(table);
-  kv.table_stride = table.has_value() ? (int32_t)table->stride(0) : 0;
+  kv.table_stride = table.has_value() ? row_step(*table) : 0;
   kv.page_size = (int32_t)k_cache.size(1);
   kv.seq_lens = (const int32_t*)seq_lens.data_ptr();
   kv.max_seq_len = max_seq_len;
@@ -326,7 +329,7 @@ fl_paged_kv paged_kv(const Tensor& cache, const Tensor& seq_lens, const OptTenso
   fl_paged_kv kv = {};
   kv.struct_size = sizeof(kv);
   kv.block_table = ptr<const int32_t>(table);
-  kv.table_stride = table.has_value() ? (int32_t)table->stride(0) : 0;
+  kv.table_stride = table.has_value() ? row_step(*table) : 0;
   kv.page_size = (int32_t)cache.size(1);
   kv.seq_lens = (const int32_t*)seq_lens.data_ptr();
   kv.max_seq_len = max_seq_len;
@@ -474,7 +477,7 @@ std::tuple<int, Tensor, Tensor, Tensor> evict(const Tensor& weights, const Tenso
   e.sinks = sinks;
   e.recent = recent;
   e.dst_table = (const int32_t*)dst_table.data_ptr();
-  e.dst_stride = (int32_t)dst_table.stride(0);
+  e.dst_stride = row_step(dst_table);
   e.new_lens = (int32_t*)lens.data_ptr();
   e.kept = (int32_t*)kept.data_ptr();
   return {fl_cache_evict(&tw, &tk, &tv, &kv, &e, &tn, (void*)stream), lens, new_weights, kept};
