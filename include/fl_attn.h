@@ -355,7 +355,7 @@ typedef struct {
 
 /* Turns q and k (either may be NULL, with its output).  The angle is reduced in 64 bits, so positions of any size keep
  * their phase; products are in 32 bits and rounded once.
- *   q  [B, 1, H, S, D],  k  [B, 1, Hkv, S, D]   bf16 or f32, one dtype; any D
+ *   q  [B, 1, H, S, D],  k  [B, 1, Hkv, S, D]   bf16 or f32, one dtype; any D; rows a multiple of 16 bytes apart, bases so aligned
  *   q_out, k_out   of the same sizes and dtype; may be q and k themselves (in place), no other overlap
  * Stream, ownership and error rules as for fl_attn_fwd; empty tensors return FL_OK without a launch. */
 fl_status fl_rotary_embed(const fl_tensor* q, const fl_tensor* k, const fl_rotary* rotary, fl_tensor* q_out, fl_tensor* k_out, void* stream);
@@ -365,9 +365,9 @@ fl_status fl_rotary_embed(const fl_tensor* q, const fl_tensor* k, const fl_rotar
  * (kv->seq_lens counts the new tokens already, as in the fl_attn_decode or fl_attn_prefill_paged call that follows).  Positions are the
  * caller's: a slot need not say where its token is in the sequence, so that a cache some tokens have been evicted from goes on as it is.
  *   q [B, 1, H, T, D], k and v [B, 1, Hkv, T, D]  bf16;  q_out as q (may be q itself);  rotary->inverse 0
- *   k_cache, v_cache, kv   as for fl_attn_decode, any D; written here.  Nothing is written for tokens at negative slots (len_b < T),
- *                          for those at slots from kv->max_seq_len on (len_b above it is not cut here) and for those whose table entry names
- *                          no page of the cache. */
+ *   k_cache, v_cache, kv   as for fl_attn_decode, any D whose rows are a multiple of 16 bytes apart; written here.  Nothing is written for
+ *                          tokens at negative slots (len_b < T), for those at slots from kv->max_seq_len on (len_b above it is not cut here)
+ *                          and for those whose table entry names no page of the cache. */
 fl_status fl_rotary_append(const fl_tensor* q, const fl_tensor* k, const fl_tensor* v, const fl_rotary* rotary, const fl_paged_kv* kv,
                            fl_tensor* q_out, fl_tensor* k_cache, fl_tensor* v_cache, void* stream);
 
@@ -376,7 +376,8 @@ fl_status fl_rotary_append(const fl_tensor* q, const fl_tensor* k, const fl_tens
  * for j < len_b: the T newest tokens start at zero, so the array needs no clearing when a sequence starts or grows.
  *   weights   [B, 1, Hkv, 1, C] f32, C >= kv->max_seq_len, unit inner stride: one row per sequence and kv head, in slot order
  *             (not in pages: sequences that share pages keep their own weights); slots from len_b on are left alone
- *   aux       workspace of fl_attn_decode_weights_workspace_size bytes
+ *   aux       workspace of fl_attn_decode_weights_workspace_size bytes, 4 of them per row, query head and token of kv->max_seq_len: a bound near
+ *             the longest sequence instead of the table's capacity keeps it small
  * Everything else, and out and lse, as for fl_attn_decode.  Results are bitwise reproducible (no atomics). */
 fl_status fl_attn_decode_weights(const fl_tensor* q, const fl_tensor* k_cache, const fl_tensor* v_cache,
                                  const fl_paged_kv* kv, const fl_variant_desc* desc, const fl_aux* aux,
@@ -420,7 +421,7 @@ typedef struct {
  * Their keys and values are copied, in slot order, to slots 0 .. of the pages in dst_table; the pages they came from are left as they are,
  * the caller's to hand out again.  Different kv heads keep different tokens: a slot of the result is no longer one position.
  *   weights       [B, 1, Hkv, 1, C] f32, C >= kv->max_seq_len, as the calls above have left them
- *   k_cache, v_cache, kv   as for fl_attn_decode (any D, bf16); with a page size that is a power of two >= 8, also without a block table
+ *   k_cache, v_cache, kv   as for fl_attn_decode (D a multiple of 8, bf16); with a page size that is a power of two >= 8, also without a block table
  *   new_weights   [B, 1, Hkv, 1, C2] f32, C2 >= budget, unit inner stride: the weights of what stays, zero from new_lens[b] to C2
  * Nothing is copied to a destination whose table entry names no page of the cache, and zeros from a source whose entry does not.
  * new_lens, kept and new_weights share no memory with one another nor with seq_lens, the tables and weights (FL_ERR_DESC): other

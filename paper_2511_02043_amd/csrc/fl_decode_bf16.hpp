@@ -15,6 +15,8 @@
 //     S^T = K Q^T and O^T += V^T P^T exactly as in the forward kernel, with the running max /
 //     sum per lane;
 //   * a page table is followed per tile row when the direct loads are issued;
+//   * P enters the second contraction as bf16, a rounding of at most 2^-8 of a probability, so that both run on the bf16 matrix instructions; its sum l
+//     and the weights of keys take the fp32 P;
 //   * waves, then splits, are merged with the rescale rule of Sec. 3.3 / 3.4 (the partial
 //     (m, l, O) of each split goes through the caller's workspace to a small second kernel).
 #pragma once
@@ -177,7 +179,8 @@ decode_kernel(const DecodeParams p) {
     return r;
   };
   // WEIGHTS: keys and values pass through the caches as data that nobody reads again (non-temporal), which leaves the scores there for the
-  // kernel behind (64 sequences of 4k - 8k tokens, 32 / 8 heads, D = 128: 372 -> 354 us, and 22.3 -> 19.6 us there)
+  // kernel behind (64 sequences of 4k - 8k tokens, 32 / 8 heads, D = 128: 372 -> 353 us in all, 22.3 -> 19.6 of them there).  Pages that sequences
+  // share are read again, and the call cannot tell: with a common prefix of 1k tokens 341 -> 347, of 4k 264 -> 329, all 8k shared 312 -> 314.
   constexpr int AUX = C::WEIGHTS ? 2 : 0;
   // all load instructions of tile t (32 keys of K, then of V) into ring stage `stage`; rows past
   // the sequence end repeat its last key (their scores are masked)
@@ -269,6 +272,7 @@ decode_kernel(const DecodeParams p) {
         mx = fmaxf(mx, a);
       }
       if constexpr (C::WEIGHTS) {
+        // (Under a soft-cap x has roundings of the cap's size, about cap * 2^-23, like the step's own probabilities, whose sums normalise it.)
         // Four keys a store; the live lanes of a tile fill whole lines together.  (64 sequences of 4k - 8k tokens, 32 / 8 heads, D = 128: 50 MB beside the
         // 1.6 GB read cost 30 of 345 us.  Scores put in the order of memory through LDS, stores a step later, and waits that leave them
         // out were 0 - 2 % faster there and slower for one sequence.)

@@ -11,7 +11,8 @@
 //     against 64 keys per wave (half the LDS reads, two waves a SIMD, 264 / 326 us in the cases below), that with the products of one block
 //     and the exponentials of the one before in a single instruction stream (244 / 298, but registers in scratch with ALiBi), and three
 //     waves a SIMD (316 / 380): 250 / 306 us for 8 chunks of 512 rows on 4k - 8k keys and for a prompt of 8192, 32 / 8 heads, D = 128.
-//     That is 0.8 - 0.9 PFLOP/s; without the exponentials 224 / 281, without the products 191 / 228;
+//     That is 0.8 - 0.9 PFLOP/s; without the exponentials 224 / 281, with one of eight products 191 / 228, without both 156 / 193.  Of the SIMDs' cycles
+//     matrix units are busy in 33 % / 42 %, vector instructions issued in 51 % / 63 %, LDS is read in 25 % / 31 % of the compute units', without conflicts;
 //   * sums over a tile's 16 registers are a tree, and only they meet the running sum: 16 times fewer roundings in the longest chain;
 //   * where few keys leave compute units idle, the (head, row tile) sequence of a key block is cut over several workgroups, whose partial
 //     sums a second kernel adds in a fixed order.
@@ -54,9 +55,9 @@ struct KeyWeightCfg : BwdCfg<D_, MOD_, 0, 64, 2> {
 // A capped score cap tanh(s / cap) is s tanh(z) / z with z = s / cap, and tanh(z) / z the cubic 1 + c1 z^2 + c2 z^4 + c3 z^6 to 2^-28 while z is
 // below kCapNear (fitted to the largest error up to there).  Beyond, cap - 2 cap / (exp(2 z) + 1): it subtracts numbers of the cap's size, so
 // that its roundings are those of scores four times as large; scores of up to 6 under a cap of 1000 would lose 10^-4 of their probabilities.  Up to a
-// cap of kCapFar those roundings are below 2^-20 for any score, and no block is asked.  (8 chunks of 512 rows on 4k - 8k keys, 32 / 8 heads, us: cap 30,
+// cap of kCapFar those roundings are about 2^-19 at most, and no block is asked.  (8 chunks of 512 rows on 4k - 8k keys, 32 / 8 heads, us: cap 30,
 // D = 128 and 64, 362 and 289, with the quotient everywhere 387 and 338; cap 12, where most blocks have a score beyond, 404 and 386; cap 5 397, and
-// 404 with blocks asked.)
+// 409 with blocks asked.)
 constexpr float kCapNear = 0.25f, kCapFar = 8.f, kCap1 = -0.33333242f, kCap2 = 0.13324264f, kCap3 = -0.05143305f;
 
 template <class C>

@@ -409,12 +409,12 @@ def rotary(q: torch.Tensor, k: Optional[torch.Tensor], positions: torch.Tensor, 
            interleaved: bool = False):
     """Rotary positions: channel pair i of every row turns by positions[b, s, axis of i] * inv_freq[i] (fl_rotary_embed).
 
-    q [B, H, S, D] and k [B, Hkv, S, D] (or None), bf16 or float32 on the GPU, any strides with unit inner stride; positions int32
-    [B, S, axes] ([1, S, axes] for all sequences alike), up to four axes such as time, height and width; inv_freq float32 [pairs],
-    2 * pairs <= D.  sections: the pairs of each axis, in order (None: one axis).  Pair i is the channels (i, i + pairs), or
-    (2i, 2i + 1) with interleaved; channels from 2 * pairs on stay.  Returns the turned q and k, in their layouts; differentiable
-    (any number of times) in both, not in inv_freq.  The backward pass reads positions and inv_freq again: changed in place before it, they
-    raise there."""
+    q [B, H, S, D] and k [B, Hkv, S, D] (or None), bf16 or float32 on the GPU, any strides with unit inner stride and rows a multiple of 16
+    bytes apart (D a multiple of 8, or of 4 in float32, since the outputs are dense); positions int32 [B, S, axes] ([1, S, axes] for all
+    sequences alike), up to four axes such as time, height and width; inv_freq float32 [pairs], 2 * pairs <= D.  sections: the pairs of each
+    axis, in order (None: one axis).  Pair i is the channels (i, i + pairs), or (2i, 2i + 1) with interleaved; channels from 2 * pairs on
+    stay.  Returns the turned q and k, in their layouts; differentiable (any number of times) in both, not in inv_freq.  The backward pass
+    reads positions and inv_freq again: changed in place before it, they raise there."""
     if not q.is_cuda or q.dtype not in (torch.bfloat16, torch.float32) or q.dim() != 4:
         raise ValueError("rotary() takes a bf16 or float32 CUDA q of shape [B, H, S, D] (there is no CPU or fallback path)")
     if getattr(inv_freq, "requires_grad", False) and _grad_enabled():
@@ -474,7 +474,9 @@ def decode_attention_weights(q: torch.Tensor, k_cache: torch.Tensor, v_cache: to
 
     q [B, H, D] (the newest token) or [B, H, T, D] (the newest T, T * H / Hkv <= 64); weights float32 [B, Hkv, capacity], capacity >=
     max_seq_len, updated in place: a key's weight grows by the probabilities that the rows and query heads of its kv head give it, and
-    starts at zero for the newest T tokens.  The rest as for decode_attention().  Returns out (and lse).  Not differentiable."""
+    starts at zero for the newest T tokens.  The rest as for decode_attention(), but the workspace: the scores wait there, 4 bytes per row, query
+    head and token of max_seq_len (by default the table's capacity: pass a bound near the longest sequence where that is much more; a
+    workspace of the caller's is contiguous memory of q's device).  Returns out (and lse).  Not differentiable."""
     if not q.is_cuda or q.dtype != torch.bfloat16 or q.dim() not in (3, 4):
         raise ValueError("decode_attention_weights() takes a bf16 CUDA q of shape [B, H, D] or [B, H, T, D]")
     status, need, out, lse = _host().decode_weights(q, k_cache, v_cache, weights, seq_lens, block_table, max_seq_len,
