@@ -2,7 +2,7 @@
  * fl_attn.h -- C ABI of the fused attention-variant library for AMD MI355X (gfx950): the forward
  * pass of every variant, the backward pass of the variants without bias, gate and second stream, and the
  * decode step (one query per sequence over a paged key/value cache); and around that cache rotary positions, the
- * weight that cached keys receive, and eviction by it.
+ * weight that cached keys receive, and eviction by it; heads normalised and turned in one pass, and the cache in 4 bits.
  *
  * One call computes, for every (b, g, h) and every query row i, without ever writing the
  * [Sq, Sk] score matrix to device memory:
@@ -53,7 +53,12 @@ typedef enum {
   FL_ERR_DESC = 10         /* descriptor fields contradict each other / bad struct_size    */
 } fl_status;
 
-typedef enum { FL_BF16 = 1, FL_F32 = 2, FL_I32 = 3 } fl_dtype;
+typedef enum {
+  FL_BF16 = 1,
+  FL_F32 = 2,
+  FL_I32 = 3,
+  FL_MX4 = 4               /* paged caches in 4 bits, see below */
+} fl_dtype;
 
 /* A strided view with logical dims [B, G, H, S, D].
  *   G is an extra independent row axis: 1 for ordinary attention, the MSA-sequence axis for
@@ -428,6 +433,77 @@ typedef struct {
  * workgroups may still have these to read. */
 fl_status fl_cache_evict(const fl_tensor* weights, fl_tensor* k_cache, fl_tensor* v_cache, const fl_paged_kv* kv, const fl_evict* evict,
                          fl_tensor* new_weights, void* stream);
+
+/* ---- heads normalised and turned in one pass; a key/value cache in 4 bits ---- */
+
+/* RMS norms of query and key heads, applied before the rotation: row x of D channels becomes  w_c x_c / sqrt(mean(x^2) + eps). */
+typedef struct {
+  uint32_t     struct_size;     /* sizeof(fl_head_norm) */
+  float        eps;             /* >= 0, finite */
+  const float* q_weight;        /* device [D], shared by the query heads; NULL: ones */
+  const float* k_weight;        /* the same for the key heads */
+} fl_head_norm;
+
+/* fl_rotary_embed of normalised heads: q and k (either may be NULL, with its output) are normalised row by row and turned, in one pass.
+ *   q  [B, 1, H, S, D],  k  [B, 1, Hkv, S, D]   bf16 or f32, one dtype; D up to 1024; rows as for fl_rotary_embed
+ *   rotary   as for fl_rotary_embed, inverse 0
+ *   q_out, k_out   of the same sizes and dtype; may be q and k themselves (in place), no other overlap
+ * Sums and products in 32 bits, rounded once. */
+fl_status fl_norm_rotary(const fl_tensor* q, const fl_tensor* k, const fl_rotary* rotary, const fl_head_norm* norm, fl_tensor* q_out, fl_tensor* k_out,
+                         void* stream);
+
+/* Its gradient.  With dz the gradient that arrives, turned back, r = 1 / sqrt(mean(x^2) + eps) and g = w dz:
+ *     dx = r g - r^3 mean(x g) x,      dw = sum over tokens and heads of r x dz
+ *   q, k             as given to fl_norm_rotary (their rows' norms are formed again)
+ *   dq_out, dk_out   the gradients that arrive, of the shapes and dtype of q and k (NULL with its input)
+ *   dq, dk           written, the same; either may be NULL: not computed
+ *   dq_weight, dk_weight   device [D] f32, written; NULL: not computed
+ *   workspace        fl_norm_rotary_bwd_workspace_size bytes, 16-byte aligned, where a weight's gradient is wanted
+ * Outputs overlap no input and not each other.  Results are bitwise reproducible (no atomics).  Without tokens dq_weight and dk_weight are zero. */
+fl_status fl_norm_rotary_bwd(const fl_tensor* q, const fl_tensor* k, const fl_tensor* dq_out, const fl_tensor* dk_out, const fl_rotary* rotary,
+                             const fl_head_norm* norm, fl_tensor* dq, fl_tensor* dk, float* dq_weight, float* dk_weight, void* workspace,
+                             size_t workspace_bytes, void* stream);
+
+/* Bytes of workspace that fl_norm_rotary_bwd needs where a weight's gradient is wanted. */
+size_t fl_norm_rotary_bwd_workspace_size(const fl_tensor* q, const fl_tensor* k, const fl_rotary* rotary);
+
+/* Keys and values in 4 bits (FL_MX4): 32 neighbouring channels of a token and kv head share a scale 2^(E - 127), E one byte, and each channel is a code of
+ * 4 bits: bit 3 the sign, bits 0 - 2 one of 0, 0.5, 1, 1.5, 2, 3, 4, 6 (e2m1 with e8m0 scales of the OCP microscaling formats).
+ * A page holds, for each kv head, the codes [page_size][D / 2] (byte i: channel 2 i in bits 0 - 3, 2 i + 1 in bits 4 - 7), then the scales [D / 32][page_size]:
+ * page_size * (D / 2 + D / 32) bytes in all, 4.25 bits a value.  D is 64 or 128, page_size a multiple of 8.
+ * The fl_tensor of such a cache has dtype FL_MX4, the sizes [pages, 1, Hkv, page_size, D] of the cache it stands for, and in stride[0] and stride[2] the BYTES
+ * from page to page and from kv head to kv head (multiples of 16); its other strides are not looked at.
+ * What enters is rounded to the nearest code, ties to the even one, under the smallest scale that every magnitude of the block is below 7 of; E is
+ * from 1 to 252, so that a held value is finite: infinities become the largest one, NaN zero.  The calls that read expect such E. */
+
+/* fl_rotary_append of normalised heads, into bf16 or 4-bit caches: writes the normalised and turned queries to q_out, and the normalised and
+ * turned keys and the values to the tokens' slots, by the rules of fl_rotary_append.
+ *   norm      NULL: no norms, turns alone
+ *   q [B, 1, H, T, D], k and v [B, 1, Hkv, T, D]  bf16;  q_out as q (may be q itself);  rotary->inverse 0
+ *   k_cache, v_cache   both bf16 (D up to 1024) or both FL_MX4.  A key that enters a 4-bit cache is computed in 64 bits: its codes are those of the exact key
+ *   k_held, v_held     NULL, or with FL_MX4 [B, 1, Hkv, T, D] bf16, written: what the cache holds for these tokens (also for those that have no
+ *                      slot), e.g. for attention among a prompt's own rows
+ * Outputs overlap no input (but q_out, as said) and not each other. */
+fl_status fl_norm_rotary_append(const fl_tensor* q, const fl_tensor* k, const fl_tensor* v, const fl_rotary* rotary, const fl_head_norm* norm,
+                                const fl_paged_kv* kv, fl_tensor* q_out, fl_tensor* k_cache, fl_tensor* v_cache, fl_tensor* k_held, fl_tensor* v_held,
+                                void* stream);
+
+/* fl_attn_decode over a 4-bit cache: the same arguments and results, with k_cache and v_cache FL_MX4.  Keys and values are bf16 numbers once their codes are
+ * read (but for scales near 2^-126), and the arithmetic from there on is that of fl_attn_decode. */
+fl_status fl_attn_decode_mx4(const fl_tensor* q, const fl_tensor* k_cache, const fl_tensor* v_cache, const fl_paged_kv* kv, const fl_variant_desc* desc,
+                             const fl_aux* aux, fl_tensor* out, fl_tensor* lse, void* stream);
+
+/* Bytes of aux->workspace that fl_attn_decode_mx4 needs. */
+size_t fl_attn_decode_mx4_workspace_size(const fl_tensor* q, const fl_tensor* k_cache, const fl_paged_kv* kv);
+
+/* fl_attn_prefill_paged over a 4-bit cache (D 64 or 128).  Chunks of so few rows that Sq * H / Hkv <= 64 are an fl_attn_decode_mx4 call; otherwise the
+ * sequences' keys and values are unpacked to dense bf16 tensors in the workspace, which the forward kernel then reads. */
+fl_status fl_attn_prefill_mx4(const fl_tensor* q, const fl_tensor* k_cache, const fl_tensor* v_cache, const fl_paged_kv* kv, const fl_variant_desc* desc,
+                              const fl_aux* aux, fl_tensor* out, fl_tensor* lse, void* stream);
+
+/* Bytes of aux->workspace that fl_attn_prefill_mx4 needs: fl_attn_decode_mx4_workspace_size for chunks of a few rows, else the dense
+ * copies, 2 * B * Hkv * max_seq_len * D * 2 bytes (each rounded up to 256). */
+size_t fl_attn_prefill_mx4_workspace_size(const fl_tensor* q, const fl_tensor* k_cache, const fl_paged_kv* kv);
 
 /* A variant compiled at run time from user expressions (opaque; owned by the caller until released). */
 typedef struct fl_custom_variant fl_custom_variant;

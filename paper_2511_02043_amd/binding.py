@@ -16,7 +16,7 @@ LIB_PATH = os.environ.get("FL_ATTN_LIB") or os.path.join(_HERE, "libflattn.so")
 # --- enums (include/fl_attn.h) -----------------------------------------------------------
 FL_OK, FL_ERR_NULL, FL_ERR_DTYPE, FL_ERR_SHAPE, FL_ERR_STRIDE, FL_ERR_ALIGN = 0, 1, 2, 3, 4, 5
 FL_ERR_UNSUPPORTED, FL_ERR_AUX_MISSING, FL_ERR_WORKSPACE, FL_ERR_LAUNCH, FL_ERR_DESC = 6, 7, 8, 9, 10
-FL_BF16, FL_F32, FL_I32 = 1, 2, 3
+FL_BF16, FL_F32, FL_I32, FL_MX4 = 1, 2, 3, 4
 FL_MOD_NONE, FL_MOD_ALIBI, FL_MOD_SOFTCAP = 0, 1, 2
 FL_MASK_CAUSAL, FL_MASK_WINDOW, FL_MASK_DOC, FL_MASK_PREFIX = 1, 2, 4, 8
 FL_SINGLE, FL_DIFFERENTIAL = 0, 1
@@ -57,6 +57,10 @@ class fl_paged_kv(C.Structure):
 class fl_rotary(C.Structure):
     _fields_ = [("struct_size", C.c_uint32), ("axes", C.c_uint32), ("sections", C.c_int32 * 4), ("interleaved", C.c_uint32),
                 ("inverse", C.c_uint32), ("positions", C.c_void_p), ("stride", C.c_int64 * 3), ("inv_freq", C.c_void_p)]
+
+
+class fl_head_norm(C.Structure):
+    _fields_ = [("struct_size", C.c_uint32), ("eps", C.c_float), ("q_weight", C.c_void_p), ("k_weight", C.c_void_p)]
 
 
 class fl_evict(C.Structure):
@@ -130,6 +134,19 @@ def lib() -> C.CDLL:
         L.fl_key_weights_workspace_size.argtypes = [TP, TP, C.POINTER(fl_paged_kv)]
         L.fl_cache_evict.restype = C.c_int
         L.fl_cache_evict.argtypes = [TP, TP, TP, C.POINTER(fl_paged_kv), C.POINTER(fl_evict), TP, C.c_void_p]
+        HN = C.POINTER(fl_head_norm)
+        L.fl_norm_rotary.restype = C.c_int
+        L.fl_norm_rotary.argtypes = [TP, TP, C.POINTER(fl_rotary), HN, TP, TP, C.c_void_p]
+        L.fl_norm_rotary_bwd.restype = C.c_int
+        L.fl_norm_rotary_bwd.argtypes = [TP, TP, TP, TP, C.POINTER(fl_rotary), HN, TP, TP, C.c_void_p, C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p]
+        L.fl_norm_rotary_bwd_workspace_size.restype = C.c_size_t
+        L.fl_norm_rotary_bwd_workspace_size.argtypes = [TP, TP, C.POINTER(fl_rotary)]
+        L.fl_norm_rotary_append.restype = C.c_int
+        L.fl_norm_rotary_append.argtypes = [TP, TP, TP, C.POINTER(fl_rotary), HN, C.POINTER(fl_paged_kv), TP, TP, TP, TP, TP, C.c_void_p]
+        L.fl_attn_decode_mx4.restype = L.fl_attn_prefill_mx4.restype = C.c_int
+        L.fl_attn_decode_mx4.argtypes = L.fl_attn_prefill_mx4.argtypes = L.fl_attn_decode.argtypes
+        L.fl_attn_decode_mx4_workspace_size.restype = L.fl_attn_prefill_mx4_workspace_size.restype = C.c_size_t
+        L.fl_attn_decode_mx4_workspace_size.argtypes = L.fl_attn_prefill_mx4_workspace_size.argtypes = [TP, TP, C.POINTER(fl_paged_kv)]
         L.fl_compile_variant.restype = C.c_int
         L.fl_compile_variant.argtypes = [C.c_char_p, C.c_char_p, C.c_uint32, C.c_int, C.POINTER(C.c_void_p)]
         L.fl_attn_fwd_custom.restype = C.c_int
@@ -172,7 +189,9 @@ def lib() -> C.CDLL:
 EXPORTS = ["fl_attn_fwd", "fl_attn_fwd_noalloc", "fl_attn_fwd_workspace_size", "fl_attn_bwd", "fl_attn_bwd_workspace_size", "fl_attn_bwd_ex", "fl_attn_bwd_ex_workspace_size",
            "fl_bwd_supported", "fl_attn_decode", "fl_attn_decode_workspace_size", "fl_attn_prefill_paged", "fl_attn_prefill_paged_workspace_size", "fl_compile_variant", "fl_attn_fwd_custom", "fl_compile_variant_aux", "fl_attn_fwd_custom_aux", "fl_attn_fwd_custom_skip", "fl_custom_skip_workspace_size", "fl_compile_variant_grad", "fl_attn_bwd_custom", "fl_attn_bwd_custom_workspace_size",
            "fl_rotary_embed", "fl_rotary_append", "fl_attn_decode_weights", "fl_attn_decode_weights_workspace_size", "fl_key_weights",
-           "fl_key_weights_workspace_size", "fl_cache_evict", "fl_release_variant", "fl_variant_supported", "fl_strerror",
+           "fl_key_weights_workspace_size", "fl_cache_evict", "fl_norm_rotary", "fl_norm_rotary_bwd", "fl_norm_rotary_bwd_workspace_size",
+           "fl_norm_rotary_append", "fl_attn_decode_mx4", "fl_attn_decode_mx4_workspace_size", "fl_attn_prefill_mx4",
+           "fl_attn_prefill_mx4_workspace_size", "fl_release_variant", "fl_variant_supported", "fl_strerror",
            "fl_last_error_detail", "fl_set_tuning", "fl_version"]
 
 
@@ -384,6 +403,69 @@ def fl_cache_evict(weights: fl_tensor, k_cache: fl_tensor, v_cache: fl_tensor, k
                    stream: int = 0) -> int:
     """Raw call; returns the fl_status code."""
     return lib().fl_cache_evict(_ref(weights), _ref(k_cache), _ref(v_cache), _ref(kv), _ref(evict), _ref(new_weights), C.c_void_p(stream))
+
+
+def head_norm(*, eps: float, q_weight=None, k_weight=None) -> fl_head_norm:
+    """Weights: float32 device tensors [D], or None for ones."""
+    n = fl_head_norm()
+    n.struct_size, n.eps = C.sizeof(fl_head_norm), eps
+    n.q_weight, n.k_weight = (None if w is None else w.data_ptr() for w in (q_weight, k_weight))
+    return n
+
+
+def mx4_desc(cache, page_size: int, D: int) -> fl_tensor:
+    """fl_tensor of a 4-bit cache, uint8 [pages, Hkv, page_size * (D / 2 + D / 32)]."""
+    t = fl_tensor()
+    t.ptr, t.dtype = cache.data_ptr(), FL_MX4
+    t.size[:] = [cache.shape[0], 1, cache.shape[1], page_size, D]
+    t.stride[:] = [cache.stride(0), 0, cache.stride(1), 0, 1]
+    return t
+
+
+def fl_norm_rotary(q: Optional[fl_tensor], k: Optional[fl_tensor], rotary: fl_rotary, norm: fl_head_norm, q_out: Optional[fl_tensor],
+                   k_out: Optional[fl_tensor], stream: int = 0) -> int:
+    """Raw call; returns the fl_status code."""
+    return lib().fl_norm_rotary(_ref(q), _ref(k), _ref(rotary), _ref(norm), _ref(q_out), _ref(k_out), C.c_void_p(stream))
+
+
+def fl_norm_rotary_bwd(q: Optional[fl_tensor], k: Optional[fl_tensor], dq_out: Optional[fl_tensor], dk_out: Optional[fl_tensor], rotary: fl_rotary,
+                       norm: fl_head_norm, dq: Optional[fl_tensor], dk: Optional[fl_tensor], dq_weight: Optional[int] = None,
+                       dk_weight: Optional[int] = None, workspace: Optional[int] = None, workspace_bytes: int = 0, stream: int = 0) -> int:
+    """Raw call (weights' gradients and workspace by address); returns the fl_status code."""
+    return lib().fl_norm_rotary_bwd(_ref(q), _ref(k), _ref(dq_out), _ref(dk_out), _ref(rotary), _ref(norm), _ref(dq), _ref(dk), C.c_void_p(dq_weight),
+                                    C.c_void_p(dk_weight), C.c_void_p(workspace), workspace_bytes, C.c_void_p(stream))
+
+
+def fl_norm_rotary_bwd_workspace_size(q: Optional[fl_tensor], k: Optional[fl_tensor], rotary: fl_rotary) -> int:
+    return lib().fl_norm_rotary_bwd_workspace_size(_ref(q), _ref(k), _ref(rotary))
+
+
+def fl_norm_rotary_append(q: fl_tensor, k: fl_tensor, v: fl_tensor, rotary: fl_rotary, norm: Optional[fl_head_norm], kv: fl_paged_kv, q_out: fl_tensor,
+                          k_cache: fl_tensor, v_cache: fl_tensor, k_held: Optional[fl_tensor] = None, v_held: Optional[fl_tensor] = None,
+                          stream: int = 0) -> int:
+    """Raw call; returns the fl_status code."""
+    return lib().fl_norm_rotary_append(_ref(q), _ref(k), _ref(v), _ref(rotary), _ref(norm), _ref(kv), _ref(q_out), _ref(k_cache), _ref(v_cache),
+                                       _ref(k_held), _ref(v_held), C.c_void_p(stream))
+
+
+def fl_attn_decode_mx4(q: fl_tensor, k_cache: fl_tensor, v_cache: fl_tensor, kv: fl_paged_kv, desc: fl_variant_desc, aux: Optional[fl_aux], out: fl_tensor,
+                       lse: Optional[fl_tensor], stream: int = 0) -> int:
+    """Raw call; returns the fl_status code."""
+    return lib().fl_attn_decode_mx4(_ref(q), _ref(k_cache), _ref(v_cache), _ref(kv), _ref(desc), _ref(aux), _ref(out), _ref(lse), C.c_void_p(stream))
+
+
+def fl_attn_decode_mx4_workspace_size(q: fl_tensor, k_cache: fl_tensor, kv: fl_paged_kv) -> int:
+    return lib().fl_attn_decode_mx4_workspace_size(_ref(q), _ref(k_cache), _ref(kv))
+
+
+def fl_attn_prefill_mx4(q: fl_tensor, k_cache: fl_tensor, v_cache: fl_tensor, kv: fl_paged_kv, desc: fl_variant_desc, aux: Optional[fl_aux], out: fl_tensor,
+                        lse: Optional[fl_tensor], stream: int = 0) -> int:
+    """Raw call; returns the fl_status code."""
+    return lib().fl_attn_prefill_mx4(_ref(q), _ref(k_cache), _ref(v_cache), _ref(kv), _ref(desc), _ref(aux), _ref(out), _ref(lse), C.c_void_p(stream))
+
+
+def fl_attn_prefill_mx4_workspace_size(q: fl_tensor, k_cache: fl_tensor, kv: fl_paged_kv) -> int:
+    return lib().fl_attn_prefill_mx4_workspace_size(_ref(q), _ref(k_cache), _ref(kv))
 
 
 def fl_compile_variant(score_mod: Optional[str], mask: Optional[str], D: int, base_mask: int = 0):

@@ -2608,3 +2608,8 @@ fl_status fl_attn_prefill_paged(const fl_tensor* q, const fl_tensor* k_cache, co
 }
 
 }  // extern "C"
+
+fl_status fl::host::forward_of_lengths(const fl_tensor* q, const fl_tensor* k, const fl_tensor* v, const fl_variant_desc* desc, const fl_aux* aux,
+                                       fl_tensor* out, fl_tensor* lse, void* stream, const int32_t* kv_lens) {
+  return forward_call(q, k, v, desc, aux, out, lse, stream, kv_lens);
+}

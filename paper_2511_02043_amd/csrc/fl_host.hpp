@@ -168,13 +168,10 @@ inline fl_status check_weights(const fl_tensor* t, const char* name, int64_t B, 
   return FL_OK;
 }
 
-// The caches [pages, 1, Hkv, page_size, D] bf16 that fl_paged_kv speaks of, B sequences of which are used.  page_shift: log2 of the page size
-// (0 where it is no power of two, which only a cache without a block table may have).
-inline fl_status check_cache(const fl_paged_kv* kv, const fl_tensor* k_cache, const fl_tensor* v_cache, int64_t B, int64_t Hkv, int64_t D,
-                             int* page_shift) {
-  if (kv == nullptr || k_cache == nullptr) return fail(FL_ERR_NULL, "kv or k_cache is NULL");
+// What fl_paged_kv says about a cache of `pages` pages, B sequences of which are used.  page_shift: log2 of the page size (0 where it is no power of
+// two, which only a cache without a block table may have).
+inline fl_status check_pages(const fl_paged_kv* kv, int64_t pages, int64_t page_size, int64_t B, int* page_shift) {
   if (kv->struct_size != sizeof(fl_paged_kv)) return fail(FL_ERR_DESC, "kv->struct_size = %u, expected %zu", kv->struct_size, sizeof(fl_paged_kv));
-  const int64_t pages = k_cache->size[0], page_size = k_cache->size[3];
   if (pages < 0 || page_size <= 0) return fail(FL_ERR_SHAPE, "negative size");
   if (pages > 0x7fffffffLL) return fail(FL_ERR_SHAPE, "more pages than an int32 table entry can name");
   if (kv->max_seq_len < 0) return fail(FL_ERR_SHAPE, "max_seq_len negative");
@@ -192,14 +189,59 @@ inline fl_status check_cache(const fl_paged_kv* kv, const fl_tensor* k_cache, co
     if (pages < B) return fail(FL_ERR_SHAPE, "without a block table the cache needs a page per sequence");
     if (kv->max_seq_len > page_size) return fail(FL_ERR_SHAPE, "max_seq_len exceeds the page size");
   }
-  if (B == 0 || Hkv == 0) return FL_OK;
+  return FL_OK;
+}
+
+// The caches [pages, 1, Hkv, page_size, D] bf16 that fl_paged_kv speaks of, B sequences of which are used.
+inline fl_status check_cache(const fl_paged_kv* kv, const fl_tensor* k_cache, const fl_tensor* v_cache, int64_t B, int64_t Hkv, int64_t D,
+                             int* page_shift) {
+  if (kv == nullptr || k_cache == nullptr) return fail(FL_ERR_NULL, "kv or k_cache is NULL");
+  const int64_t pages = k_cache->size[0], page_size = k_cache->size[3];
+  fl_status st = check_pages(kv, pages, page_size, B, page_shift);
+  if (st != FL_OK || B == 0 || Hkv == 0) return st;
   if (kv->seq_lens == nullptr) return fail(FL_ERR_NULL, "seq_lens is NULL");
   const int64_t size[5] = {pages, 1, Hkv, page_size, D};
-  fl_status st = FL_OK;
   if (kv->max_seq_len > 0 && (st = check_data_tensor(k_cache, "k_cache", FL_BF16, size)) == FL_OK && v_cache != nullptr)
     st = check_data_tensor(v_cache, "v_cache", FL_BF16, size);
   return st;
 }
+
+// The same of caches in 4 bits: FL_MX4, of which only the strides of pages and kv heads, in bytes, say anything.
+inline fl_status check_cache_mx4(const fl_paged_kv* kv, const fl_tensor* k_cache, const fl_tensor* v_cache, int64_t B, int64_t Hkv, int64_t D,
+                                 int* page_shift) {
+  if (kv == nullptr || k_cache == nullptr || v_cache == nullptr) return fail(FL_ERR_NULL, "kv, k_cache or v_cache is NULL");
+  if (D != 64 && D != 128) return fail(FL_ERR_UNSUPPORTED, "D = %lld: caches in 4 bits take 64 or 128", (long long)D);
+  const int64_t pages = k_cache->size[0], page_size = k_cache->size[3];
+  fl_status st = check_pages(kv, pages, page_size, B, page_shift);
+  if (st != FL_OK) return st;
+  if (page_size % 8 != 0 || page_size > (1 << 24))
+    return fail(FL_ERR_SHAPE, "pages of %lld tokens: caches in 4 bits take multiples of 8 up to 2^24", (long long)page_size);
+  if (B == 0 || Hkv == 0) return FL_OK;
+  if (kv->seq_lens == nullptr) return fail(FL_ERR_NULL, "seq_lens is NULL");
+  if (kv->max_seq_len == 0) return FL_OK;
+  const int64_t size[5] = {pages, 1, Hkv, page_size, D}, bytes = page_size * (D / 2 + D / 32);
+  for (int w = 0; w < 2; ++w) {
+    const fl_tensor* t = w ? v_cache : k_cache;
+    const char* name = w ? "v_cache" : "k_cache";
+    if (t->ptr == nullptr) return fail(FL_ERR_NULL, "%s is NULL", name);
+    if (t->dtype != FL_MX4) return fail(FL_ERR_DTYPE, "%s has dtype %d, expected %d", name, t->dtype, FL_MX4);
+    for (int a = 0; a < 5; ++a)
+      if (t->size[a] != size[a])
+        return fail(FL_ERR_SHAPE, "%s size[%d] = %lld, expected %lld", name, a, (long long)t->size[a], (long long)size[a]);
+    if (((uintptr_t)t->ptr) % 16 != 0) return fail(FL_ERR_ALIGN, "%s base pointer not 16-byte aligned", name);
+    for (int a = 0; a < 4; a += 2) {
+      if (t->size[a] <= 1) continue;
+      if (t->stride[a] < bytes) return fail(FL_ERR_STRIDE, "%s stride[%d] = %lld is less than a page and head's %lld bytes", name, a, (long long)t->stride[a], (long long)bytes);
+      if (t->stride[a] % 16 != 0) return fail(FL_ERR_ALIGN, "%s stride[%d] not a multiple of 16 bytes", name, a);
+    }
+    if (rows_overlap(Hkv, t->stride[2], pages, t->stride[0], bytes)) return fail(FL_ERR_STRIDE, "%s strides: pages overlap", name);
+  }
+  return FL_OK;
+}
+
+// The forward pass behind fl_attn_fwd on keys and values [B, 1, Hkv, L, D] of which sequence b has kv_lens[b] (device): its query rows are the last of those.
+fl_status forward_of_lengths(const fl_tensor* q, const fl_tensor* k, const fl_tensor* v, const fl_variant_desc* desc, const fl_aux* aux, fl_tensor* out,
+                             fl_tensor* lse, void* stream, const int32_t* kv_lens);
 
 }  // namespace host
 }  // namespace fl

@@ -1,0 +1,222 @@
+// C-ABI entry points of attention over a paged cache in 4 bits: the decode step and a chunk of query rows.  Argument validation and launch; the
+// arithmetic is in fl_mx4_decode.hpp and, for chunks, in the forward kernels.
+#include <algorithm>
+#include <cstring>
+
+#include "fl_host.hpp"
+#include "fl_mx4_decode.hpp"
+
+namespace {
+
+using namespace fl::host;
+
+constexpr int64_t kMostPairs = 64;                 // (query row, head) pairs of a kv head: four column blocks of 16
+
+// Splits of a sequence's keys, from the shapes and the host-side bound of the lengths alone.
+int splits_of(int64_t B, int64_t Hkv, int64_t max_seq_len) {
+  const int64_t tiles = (max_seq_len + 31) / 32, units = std::max<int64_t>(1, B * Hkv);
+  const int64_t want = std::min<int64_t>({(1024 + units - 1) / units, tiles / 4, 64});
+  return (int)std::max<int64_t>(1, want);
+}
+
+size_t decode_bytes(int64_t B, int64_t T, int64_t H, int64_t D, int ns) { return (size_t)(B * T * H * ns) * (size_t)(D + 2) * sizeof(float); }
+
+template <int D, int MOD>
+hipError_t launch_decode(const fl::Mx4DecodeParams& p, int blocks, int pairs, hipStream_t stream) {
+  if (pairs <= 16) hipLaunchKernelGGL((fl::mx4_decode_kernel<D, MOD, 1>), dim3(blocks), dim3(256), 0, stream, p);
+  else if (pairs <= 32) hipLaunchKernelGGL((fl::mx4_decode_kernel<D, MOD, 2>), dim3(blocks), dim3(256), 0, stream, p);
+  else hipLaunchKernelGGL((fl::mx4_decode_kernel<D, MOD, 4>), dim3(blocks), dim3(256), 0, stream, p);
+  return hipGetLastError();
+}
+template <int D>
+hipError_t launch_decode(uint32_t mod, const fl::Mx4DecodeParams& p, int blocks, int pairs, hipStream_t stream) {
+  const hipError_t e = mod == FL_MOD_NONE    ? launch_decode<D, fl::kModNone>(p, blocks, pairs, stream)
+                       : mod == FL_MOD_ALIBI ? launch_decode<D, fl::kModAlibi>(p, blocks, pairs, stream)
+                                             : launch_decode<D, fl::kModSoftcap>(p, blocks, pairs, stream);
+  if (e != hipSuccess || p.nsplit == 1) return e;
+  hipLaunchKernelGGL(fl::decode_combine_kernel<D>, dim3(p.B * p.T * p.H), dim3(64), 0, stream, p);
+  return hipGetLastError();
+}
+
+fl::Mx4Cache cache_of(const fl_tensor* k_cache, const fl_tensor* v_cache, const fl_paged_kv* kv) {
+  const fl::View k = make_view(k_cache), v = make_view(v_cache);
+  return {(uint8_t*)k_cache->ptr, (uint8_t*)v_cache->ptr, k.sb, k.sh, v.sb, v.sh, kv->page_size};
+}
+
+// What both calls check; `name` in messages.
+fl_status check_call(const char* name, const fl_tensor* q, const fl_tensor* k_cache, const fl_tensor* v_cache, const fl_paged_kv* kv, const fl_variant_desc* desc,
+                     const fl_aux* aux, const fl_tensor* out, const fl_tensor* lse, int* page_shift, bool* empty) {
+  fl_status st = check_desc(desc);
+  if (st != FL_OK) return st;
+  if (q == nullptr || k_cache == nullptr || v_cache == nullptr || kv == nullptr || out == nullptr) return fail(FL_ERR_NULL, "q, k_cache, v_cache, kv or out is NULL");
+  if (aux != nullptr && aux->struct_size != sizeof(fl_aux)) return fail(FL_ERR_DESC, "aux->struct_size = %u, expected %zu", aux->struct_size, sizeof(fl_aux));
+  const uint32_t mask = canonical_mask(desc->mask);
+  if ((mask & (FL_MASK_DOC | FL_MASK_PREFIX)) || desc->n_bias != 0 || desc->combine != FL_SINGLE || desc->epilogue != 0 || desc->q_offset != 0)
+    return fail(FL_ERR_UNSUPPORTED, "%s covers scale, score_mod and the sliding window only", name);
+  if (q->dtype != FL_BF16) return fail(FL_ERR_DTYPE, "%s takes a bf16 q (dtype %d)", name, q->dtype);
+  const int64_t B = q->size[0], H = q->size[2], T = q->size[3], D = q->size[4], Hkv = k_cache->size[2];
+  if (B < 0 || H < 0 || T < 0 || D <= 0 || Hkv < 0) return fail(FL_ERR_SHAPE, "negative size");
+  if (q->size[1] != 1) return fail(FL_ERR_SHAPE, "q must be [B, 1, H, rows, D]");
+  if (T > 0x3fffffff) return fail(FL_ERR_SHAPE, "more than 2^30 rows");
+  if (H != 0 && (Hkv <= 0 || H % Hkv != 0)) return fail(FL_ERR_SHAPE, "kv heads (%lld) must divide q heads (%lld)", (long long)Hkv, (long long)H);
+  if ((st = check_cache_mx4(kv, k_cache, v_cache, B, Hkv, D, page_shift)) != FL_OK) return st;
+  *empty = B == 0 || H == 0 || T == 0;
+  if (*empty) return FL_OK;
+  const int64_t qs[5] = {B, 1, H, T, D}, ls[5] = {B, 1, H, T, 1};
+  if ((st = check_data_tensor(q, "q", FL_BF16, qs)) != FL_OK) return st;
+  if (out->dtype != FL_BF16 && out->dtype != FL_F32) return fail(FL_ERR_DTYPE, "out dtype %d", out->dtype);
+  if ((st = check_data_tensor(out, "out", out->dtype, qs)) != FL_OK) return st;
+  if (lse != nullptr && lse->ptr != nullptr) {
+    if (lse->dtype != FL_F32) return fail(FL_ERR_DTYPE, "lse must be f32");
+    for (int a = 0; a < 5; ++a)
+      if (lse->size[a] != ls[a]) return fail(FL_ERR_SHAPE, "lse size[%d] = %lld, expected %lld", a, (long long)lse->size[a], (long long)ls[a]);
+  }
+  if (aux == nullptr) return fail(FL_ERR_AUX_MISSING, "%s needs aux (workspace)", name);
+  if (desc->score_mod == FL_MOD_ALIBI && aux->alibi_slopes == nullptr) return fail(FL_ERR_AUX_MISSING, "alibi_slopes");
+  return FL_OK;
+}
+
+fl_status check_workspace(const fl_aux* aux, size_t need) {
+  if (aux->workspace == nullptr || aux->workspace_bytes < need)
+    return fail(FL_ERR_WORKSPACE, "workspace needs %zu bytes, got %zu", need, aux->workspace ? aux->workspace_bytes : (size_t)0);
+  if (((uintptr_t)aux->workspace) % 16 != 0) return fail(FL_ERR_ALIGN, "workspace not 16-byte aligned");
+  return FL_OK;
+}
+
+// The decode step, its arguments checked.
+fl_status decode(const fl_tensor* q, const fl_tensor* k_cache, const fl_tensor* v_cache, const fl_paged_kv* kv, const fl_variant_desc* desc, const fl_aux* aux,
+                 fl_tensor* out, fl_tensor* lse, int page_shift, hipStream_t stream) {
+  const int64_t B = q->size[0], H = q->size[2], T = q->size[3], D = q->size[4], Hkv = k_cache->size[2];
+  const int ns = splits_of(B, Hkv, kv->max_seq_len);
+  const fl_status st = check_workspace(aux, decode_bytes(B, T, H, D, ns));
+  if (st != FL_OK) return st;
+  if (B * Hkv * ns > 0x7fffffffLL || B * T * H > 0x7fffffffLL) return fail(FL_ERR_SHAPE, "too many workgroups");
+  const uint32_t mask = canonical_mask(desc->mask);
+  fl::Mx4DecodeParams p;
+  memset(&p, 0, sizeof(p));
+  const fl::View qv = make_view(q), ov = make_view(out);
+  p.q = (const uint16_t*)q->ptr;
+  p.q_sb = qv.sb; p.q_sh = qv.sh; p.q_st = qv.ss;
+  p.cache = cache_of(k_cache, v_cache, kv);
+  p.block_table = kv->block_table;
+  p.table_stride = kv->table_stride;
+  p.page_shift = page_shift;
+  p.num_pages = (int)k_cache->size[0];
+  p.seq_lens = kv->seq_lens;
+  p.max_len = kv->max_seq_len;
+  p.out = out->ptr;
+  p.o_sb = ov.sb; p.o_sh = ov.sh; p.o_st = ov.ss;
+  p.out_f32 = out->dtype == FL_F32;
+  if (lse != nullptr && lse->ptr != nullptr) {
+    const fl::View lv = make_view(lse);
+    p.lse = (float*)lse->ptr;
+    p.lse_sb = lv.sb; p.lse_sh = lv.sh; p.lse_st = lv.ss;
+  }
+  p.part_o = (float*)aux->workspace;
+  p.part_ml = p.part_o + B * T * H * ns * D;
+  p.alibi_slopes = aux->alibi_slopes;
+  p.B = (int)B; p.H = (int)H; p.Hkv = (int)Hkv; p.T = (int)T;
+  p.nsplit = ns;
+  p.by_split = fl::Divisor::of(ns);
+  p.by_hkv = fl::Divisor::of(Hkv);
+  p.by_group = fl::Divisor::of(H / Hkv);
+  p.by_h = fl::Divisor::of(H);
+  p.by_t = fl::Divisor::of(T);
+  p.window = (mask & FL_MASK_WINDOW) ? clamp_window(desc->window, kv->max_seq_len, kv->max_seq_len) : -1;
+  p.scale = desc->scale;
+  p.softcap = std::fmin(std::fmax(desc->softcap, 0x1p-120f), 0x1p120f);   // (both and twice them finite; beyond them every score is 0 in fp32, as at them)
+  const int blocks = (int)(B * Hkv * ns), pairs = (int)(T * (H / Hkv));
+  const hipError_t e = D == 128 ? launch_decode<128>(desc->score_mod, p, blocks, pairs, stream) : launch_decode<64>(desc->score_mod, p, blocks, pairs, stream);
+  return e == hipSuccess ? FL_OK : fail(FL_ERR_LAUNCH, "decode launch: %s", hipGetErrorString(e));
+}
+
+bool few_rows(int64_t H, int64_t Hkv, int64_t Sq) { return Hkv > 0 && Sq <= kMostPairs && Sq * (H / Hkv) <= kMostPairs; }
+
+size_t dense_bytes(int64_t B, int64_t Hkv, int64_t D, int64_t max_len) {
+  return ((size_t)(B * Hkv * std::max<int64_t>(max_len, 1) * D) * 2 + 255) / 256 * 256;
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t fl_attn_decode_mx4_workspace_size(const fl_tensor* q, const fl_tensor* k_cache, const fl_paged_kv* kv) {
+  if (q == nullptr || k_cache == nullptr || kv == nullptr) return 0;
+  return decode_bytes(q->size[0], q->size[3], q->size[2], q->size[4], splits_of(q->size[0], k_cache->size[2], kv->max_seq_len));
+}
+
+fl_status fl_attn_decode_mx4(const fl_tensor* q, const fl_tensor* k_cache, const fl_tensor* v_cache, const fl_paged_kv* kv, const fl_variant_desc* desc,
+                             const fl_aux* aux, fl_tensor* out, fl_tensor* lse, void* stream) {
+  clear_detail();
+  int page_shift = 0;
+  bool empty = false;
+  const fl_status st = check_call("the decode step over 4 bits", q, k_cache, v_cache, kv, desc, aux, out, lse, &page_shift, &empty);
+  if (st != FL_OK) return st;
+  if (q->size[2] != 0 && !few_rows(q->size[2], k_cache->size[2], q->size[3]))
+    return fail(FL_ERR_SHAPE, "at most %lld (query row, q head) pairs per kv head (T = %lld)", (long long)kMostPairs, (long long)q->size[3]);
+  if (empty) return FL_OK;
+  return decode(q, k_cache, v_cache, kv, desc, aux, out, lse, page_shift, (hipStream_t)stream);
+}
+
+size_t fl_attn_prefill_mx4_workspace_size(const fl_tensor* q, const fl_tensor* k_cache, const fl_paged_kv* kv) {
+  if (q == nullptr || k_cache == nullptr || kv == nullptr) return 0;
+  if (few_rows(q->size[2], k_cache->size[2], q->size[3])) return fl_attn_decode_mx4_workspace_size(q, k_cache, kv);
+  return 2 * dense_bytes(q->size[0], k_cache->size[2], q->size[4], kv->max_seq_len);
+}
+
+fl_status fl_attn_prefill_mx4(const fl_tensor* q, const fl_tensor* k_cache, const fl_tensor* v_cache, const fl_paged_kv* kv, const fl_variant_desc* desc,
+                              const fl_aux* aux, fl_tensor* out, fl_tensor* lse, void* stream_v) {
+  clear_detail();
+  int page_shift = 0;
+  bool empty = false;
+  fl_status st = check_call("prefill over 4 bits", q, k_cache, v_cache, kv, desc, aux, out, lse, &page_shift, &empty);
+  if (st != FL_OK || empty) return st;
+  hipStream_t stream = (hipStream_t)stream_v;
+  const int64_t B = q->size[0], H = q->size[2], Sq = q->size[3], D = q->size[4], Hkv = k_cache->size[2], L = kv->max_seq_len;
+  if (few_rows(H, Hkv, Sq)) return decode(q, k_cache, v_cache, kv, desc, aux, out, lse, page_shift, stream);
+
+  // the inner forward call: causal, every sequence's key count read on the device.  What it can refuse is checked before the first launch.
+  fl_variant_desc inner = *desc;
+  inner.mask = canonical_mask(desc->mask) | FL_MASK_CAUSAL;
+  fl_aux ia;
+  memset(&ia, 0, sizeof(ia));
+  ia.struct_size = sizeof(fl_aux);
+  ia.alibi_slopes = aux->alibi_slopes;
+  if (!fl_variant_supported(&inner, FL_BF16, (int)D, (int)D)) return fail(FL_ERR_UNSUPPORTED, "no forward kernel for D=%lld score_mod=%u with this mask", (long long)D, desc->score_mod);
+  const size_t half = dense_bytes(B, Hkv, D, L);
+  if ((st = check_workspace(aux, 2 * half)) != FL_OK) return st;
+  const int64_t total = B * Hkv * L * (D / 32);
+  if ((total + 255) / 256 > 0x7fffffffLL) return fail(FL_ERR_SHAPE, "too many rows to unpack");
+  fl_tensor kd, vd;
+  memset(&kd, 0, sizeof(kd));
+  kd.dtype = FL_BF16;
+  kd.size[0] = B; kd.size[1] = 1; kd.size[2] = Hkv; kd.size[3] = L; kd.size[4] = D;
+  kd.stride[4] = 1; kd.stride[3] = D; kd.stride[2] = L * D; kd.stride[1] = Hkv * L * D; kd.stride[0] = Hkv * L * D;
+  vd = kd;
+  kd.ptr = aux->workspace;
+  vd.ptr = (char*)aux->workspace + half;
+  if (total > 0) {
+    fl::Mx4UnpackParams u;
+    memset(&u, 0, sizeof(u));
+    u.cache = cache_of(k_cache, v_cache, kv);
+    u.dst[0] = (uint16_t*)kd.ptr;
+    u.dst[1] = (uint16_t*)vd.ptr;
+    u.block_table = kv->block_table;
+    u.seq_lens = kv->seq_lens;
+    u.table_stride = kv->table_stride;
+    u.page_shift = page_shift;
+    u.num_pages = (int)k_cache->size[0];
+    u.max_len = kv->max_seq_len;
+    u.Hkv = (int)Hkv;
+    u.L = (int)L;
+    u.D = (int)D;
+    u.blocks = (int)(D / 32);
+    u.total = total;
+    hipLaunchKernelGGL(fl::mx4_unpack_kernel, dim3((unsigned)((total + 255) / 256), 2), dim3(256), 0, stream, u);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return fail(FL_ERR_LAUNCH, "unpack launch: %s", hipGetErrorString(e));
+  }
+  return forward_of_lengths(q, &kd, &vd, &inner, &ia, out, lse, stream_v, kv->seq_lens);
+}
+
+}  // extern "C"

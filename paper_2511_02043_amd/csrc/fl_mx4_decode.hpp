@@ -1,0 +1,303 @@
+// Attention over a paged cache in 4 bits for gfx950: the decode step, and the unpacked copy that a long chunk of queries reads.
+#pragma once
+#include "fl_decode_bf16.hpp"
+#include "fl_mx4.hpp"
+
+namespace fl {
+
+typedef __attribute__((ext_vector_type(4))) float f32x4;
+
+// Every sequence's cached rows as dense bf16 tensors [B, Hkv, L, D], row j token j, for the forward kernel that a long chunk of queries runs through.
+// Rows from a sequence's length on are left as they are: that kernel is told the length.  A thread has a block of 32 channels of a key or
+// a value (blockIdx.y): 17 bytes in, 64 out.
+struct Mx4UnpackParams {
+  Mx4Cache cache;
+  uint16_t* dst[2];
+  const int32_t* block_table;
+  const int32_t* seq_lens;
+  int32_t table_stride, page_shift, num_pages, max_len, Hkv, L, D, blocks;           // blocks = D / 32
+  int64_t total;                                                                     // B * Hkv * L * blocks
+};
+__global__ void __launch_bounds__(256) mx4_unpack_kernel(const Mx4UnpackParams p) {
+  const int64_t idx = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  if (idx >= p.total) return;
+  const int blk = (int)(idx % p.blocks);
+  int64_t rest = idx / p.blocks;
+  const int j = (int)(rest % p.L);
+  rest /= p.L;
+  const int hk = (int)(rest % p.Hkv), b = (int)(rest / p.Hkv);
+  const int len = min(max(p.seq_lens[b], 0), p.max_len);
+  if (j >= len) return;
+  int64_t page = b;
+  int within = j;
+  if (p.block_table != nullptr) {
+    page = min(max(p.block_table[(int64_t)b * p.table_stride + (j >> p.page_shift)], 0), p.num_pages - 1);
+    within = j & ((1 << p.page_shift) - 1);
+  }
+  const bool values = blockIdx.y != 0;
+  const uint8_t* at = values ? p.cache.v + page * p.cache.v_sp + hk * p.cache.v_sh : p.cache.k + page * p.cache.k_sp + hk * p.cache.k_sh;
+  const uint4 codes = *(const uint4*)(at + (int64_t)within * (p.D / 2) + blk * 16);
+  const float scale = mx4_scale_value(at[(int64_t)p.cache.page_size * (p.D / 2) + (int64_t)blk * p.cache.page_size + within]);
+  uint4* to = (uint4*)(p.dst[values ? 1 : 0] + idx * 32);
+  to[0] = mx4_bf16x8(codes.x, scale);
+  to[1] = mx4_bf16x8(codes.y, scale);
+  to[2] = mx4_bf16x8(codes.z, scale);
+  to[3] = mx4_bf16x8(codes.w, scale);
+}
+
+// ---- the decode step over a cache in 4 bits ----
+
+struct Mx4DecodeParams : DecodeParams {
+  Mx4Cache cache;                  // in place of k, v and their strides
+};
+
+// max and sum over the four lanes of a column (16 apart)
+__device__ __forceinline__ float quarter_max(float x) {
+  x = fmaxf(x, __shfl_xor(x, 16));
+  return fmaxf(x, __shfl_xor(x, 32));
+}
+__device__ __forceinline__ float quarter_sum(float x) {
+  x += __shfl_xor(x, 16);
+  return x + __shfl_xor(x, 32);
+}
+
+// A workgroup owns one (sequence, kv head, split of the key range); its four waves take tiles of 32 keys in turn.  NB blocks of 16
+// (query row, head) pairs are the columns of the matrix products, S^T = K Q^T and O^T += V^T P^T on 16 x 16 x 32 instructions:
+//   * lane = (g, m), g = lane / 16.  The order of a contraction's terms is free, so that a lane's codes of one key are a quarter of its row in
+//     one load, channels D/4 g + 8 s + .. in step s, and its block's scale goes into the conversion;
+//   * row m of product u = 0, 1 is key 8 (m / 4) + 4 u + m % 4 of the tile.  A lane's scores are then those of keys 8 g .. 8 g + 7 in order, which
+//     is what the second contraction wants of P: no exchange between lanes;
+//   * for that one, a lane has keys 8 g .. + 7 of channels D/16 m .. + D/16 - 1: the codes of two keys are converted two channels at a time, then
+//     paired key by key.
+template <int D, int MOD, int NB>
+__global__ void __launch_bounds__(256) mx4_decode_kernel(const Mx4DecodeParams p) {
+  constexpr int KS = D / 32;                       // steps of the first contraction
+  constexpr int CH = D / 16;                       // channels of a lane in the second
+  __shared__ float park[4][CH * 4 * 64];
+  __shared__ float2 park_ml[4][64];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = lane >> 4, m = lane & 15;
+
+  int split, bhk, hk, b;
+  p.by_split.split(blockIdx.x, bhk, split);
+  p.by_hkv.split(bhk, b, hk);
+  const int group = (int)p.by_group.d, ncol = p.T * group;
+  const int len = min(max(p.seq_lens[b], 0), p.max_len);
+  int row[NB], hq[NB], pos[NB];
+  bool live[NB];
+#pragma unroll
+  for (int nb = 0; nb < NB; ++nb) {
+    const int c = 16 * nb + m;
+    live[nb] = c < ncol;
+    int head;
+    p.by_group.split(live[nb] ? c : ncol - 1, row[nb], head);
+    hq[nb] = hk * group + head;
+    pos[nb] = len - p.T + row[nb];
+  }
+  const int first_key = p.window >= 0 ? max(0, len - p.T - p.window) : 0;
+  const int first_full = p.window >= 0 ? max(0, len - 1 - p.window) : 0;
+  const int t_lo = first_key / 32, t_hi = (len + 31) / 32;
+  const int per_split = p.by_split.div(t_hi - t_lo + p.nsplit - 1);
+  const int t_begin = t_lo + split * per_split, t_end = min(t_hi, t_begin + per_split);
+
+  bf16x8 qf[NB][KS];
+  float slope2[NB], m_run[NB], l_run[NB];
+  f32x4 oacc[NB][CH];
+#pragma unroll
+  for (int nb = 0; nb < NB; ++nb) {
+    const uint16_t* qp = p.q + b * p.q_sb + hq[nb] * p.q_sh + row[nb] * p.q_st + g * (D / 4);
+#pragma unroll
+    for (int s = 0; s < KS; ++s) qf[nb][s] = *(const bf16x8*)(qp + 8 * s);
+    slope2[nb] = MOD == kModAlibi ? p.alibi_slopes[hq[nb]] * kLog2e : 0.f;
+    m_run[nb] = -INFINITY;
+    l_run[nb] = 0.f;
+#pragma unroll
+    for (int c = 0; c < CH; ++c) oacc[nb][c] = (f32x4){0.f, 0.f, 0.f, 0.f};
+  }
+  const float c_scale = p.scale * kLog2e;
+  const int64_t codes_bytes = (int64_t)p.cache.page_size * (D / 2);
+
+  for (int t = t_begin + wave; t < t_end; t += 4) {
+    // the pages of this lane's eight keys in either contraction (an octet lies in one page; behind the sequence: its last one)
+    const uint8_t *kp, *vp;
+    int k_in, v_in;
+    auto octet = [&](int o, const uint8_t* base, int64_t sp, int64_t sh, int& within) __attribute__((always_inline)) {
+      const int j = min(t * 32 + 8 * o, (len - 1) & ~7);
+      int64_t page = b;
+      within = j;
+      if (p.block_table != nullptr) {
+        page = min(max(p.block_table[(int64_t)b * p.table_stride + (j >> p.page_shift)], 0), p.num_pages - 1);
+        within = j & ((1 << p.page_shift) - 1);
+      }
+      return base + page * sp + hk * sh;
+    };
+    kp = octet(m >> 2, p.cache.k, p.cache.k_sp, p.cache.k_sh, k_in);
+    vp = octet(g, p.cache.v, p.cache.v_sp, p.cache.v_sh, v_in);
+    uint32_t kc[2][KS], vc[8];
+    int ke[2];
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      const int j = k_in + 4 * u + (m & 3);
+      if constexpr (D == 128) {
+        const uint4 x = *(const uint4*)(kp + (int64_t)j * (D / 2) + g * (D / 8));
+        kc[u][0] = x.x; kc[u][1] = x.y; kc[u][2] = x.z; kc[u][3] = x.w;
+      } else {
+        const uint2 x = *(const uint2*)(kp + (int64_t)j * (D / 2) + g * (D / 8));
+        kc[u][0] = x.x; kc[u][1] = x.y;
+      }
+      ke[u] = kp[codes_bytes + (int64_t)(g * (D / 4) / 32) * p.cache.page_size + j];
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const uint8_t* at = vp + (int64_t)(v_in + i) * (D / 2) + m * (CH / 2);
+      if constexpr (D == 128) vc[i] = *(const uint32_t*)at;
+      else vc[i] = *(const uint16_t*)at;
+    }
+    uint2 ve = *(const uint2*)(vp + codes_bytes + (int64_t)(m * CH / 32) * p.cache.page_size + v_in);
+
+    f32x4 s[NB][2];
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+#pragma unroll
+      for (int nb = 0; nb < NB; ++nb) s[nb][u] = (f32x4){0.f, 0.f, 0.f, 0.f};
+      const float scale = mx4_scale_value(ke[u]);
+#pragma unroll
+      for (int f = 0; f < KS; ++f) {
+        const bf16x8 a = __builtin_bit_cast(bf16x8, mx4_bf16x8(kc[u][f], scale));
+#pragma unroll
+        for (int nb = 0; nb < NB; ++nb) s[nb][u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, qf[nb][f], s[nb][u], 0, 0, 0);
+      }
+    }
+    const int jb = t * 32 + 8 * g;
+    const bool partial = t * 32 + 32 > len - p.T + 1 || t * 32 < first_full;       // uniform
+    bf16x8 pf[NB];
+#pragma unroll
+    for (int nb = 0; nb < NB; ++nb) {
+      const int lo_key = p.window >= 0 ? pos[nb] - p.window : 0;
+      float x[8], mx = -INFINITY;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const int j = jb + i;
+        const float raw = s[nb][i >> 2][i & 3];
+        float a;
+        if constexpr (MOD == kModSoftcap) {
+          const float e = fast_exp2(raw * (2.f * c_scale / p.softcap));
+          a = fmaf(fast_rcp(e + 1.f), -2.f * p.softcap * kLog2e, p.softcap * kLog2e);
+        } else if constexpr (MOD == kModAlibi) {
+          a = fmaf(raw, c_scale, -slope2[nb] * (float)(pos[nb] - j));
+        } else {
+          a = raw * c_scale;
+        }
+        if (partial && (j > pos[nb] || j < lo_key)) a = -INFINITY;
+        x[i] = a;
+        mx = fmaxf(mx, a);
+      }
+      // as in the step over bf16 pages the running maximum moves only where a score exceeds it by 2^8, here before any lane has
+      // looked at the column's others
+      if (__builtin_amdgcn_ballot_w64(mx - m_run[nb] > kLazyMaxLog2) != 0) {
+        mx = quarter_max(mx);
+        const float m_new = (mx - m_run[nb] > kLazyMaxLog2) ? mx : m_run[nb];
+        const float alpha = m_new != m_run[nb] ? fast_exp2(m_run[nb] - m_new) : 1.f;
+        m_run[nb] = m_new;
+        l_run[nb] *= alpha;
+#pragma unroll
+        for (int c = 0; c < CH; ++c)
+#pragma unroll
+          for (int r = 0; r < 4; ++r) oacc[nb][c][r] *= alpha;
+      }
+      const float m_safe = m_run[nb] == -INFINITY ? 0.f : m_run[nb];
+      float psum = 0.f;
+      uint32_t pw[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const float p0 = fast_exp2(x[2 * i] - m_safe), p1 = fast_exp2(x[2 * i + 1] - m_safe);
+        psum += p0 + p1;
+        pw[i] = pack_bf16(p0, p1);
+      }
+      l_run[nb] += psum;
+      pf[nb] = __builtin_bit_cast(bf16x8, (i32x4){(int)pw[0], (int)pw[1], (int)pw[2], (int)pw[3]});
+    }
+    float vs[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const int e = ((i < 4 ? ve.x : ve.y) >> (8 * (i & 3))) & 255;
+      // what lies behind the sequence's end in its last page is any bytes: finite, for P is zero there
+      vs[i] = t * 32 + 8 * g + i < len ? mx4_scale_value(e) : 1.f;
+    }
+#pragma unroll
+    for (int f = 0; f < CH / 2; ++f) {
+      uint32_t c[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        bf16x2 y;
+        if (f == 0) y = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(vc[i], vs[i], 0);
+        else if (f == 1) y = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(vc[i], vs[i], 1);
+        else if (f == 2) y = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(vc[i], vs[i], 2);
+        else y = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(vc[i], vs[i], 3);
+        c[i] = __builtin_bit_cast(uint32_t, y);
+      }
+      i32x4 lo, hi;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        lo[i] = (int)__builtin_amdgcn_perm(c[2 * i + 1], c[2 * i], 0x05040100u);
+        hi[i] = (int)__builtin_amdgcn_perm(c[2 * i + 1], c[2 * i], 0x07060302u);
+      }
+#pragma unroll
+      for (int nb = 0; nb < NB; ++nb) {
+        oacc[nb][2 * f] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, lo), pf[nb], oacc[nb][2 * f], 0, 0, 0);
+        oacc[nb][2 * f + 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, hi), pf[nb], oacc[nb][2 * f + 1], 0, 0, 0);
+      }
+    }
+  }
+
+  // ---- merge of the waves, a column block at a time; wave i then holds channels CH (4 g + i) .. + CH - 1 of column m
+#pragma unroll
+  for (int nb = 0; nb < NB; ++nb) {
+    if (nb > 0) __syncthreads();
+#pragma unroll
+    for (int c = 0; c < CH; ++c)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) park[wave][(c * 4 + r) * 64 + lane] = oacc[nb][c][r];
+    park_ml[wave][lane] = make_float2(m_run[nb], quarter_sum(l_run[nb]));
+    __syncthreads();
+    float m_all = -INFINITY, l_all = 0.f, wgt[4];
+#pragma unroll
+    for (int u = 0; u < 4; ++u) m_all = fmaxf(m_all, park_ml[u][lane].x);
+    const float m_safe = m_all == -INFINITY ? 0.f : m_all;
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      const float2 ml = park_ml[u][lane];
+      wgt[u] = fast_exp2(ml.x - m_safe);
+      l_all = fmaf(ml.y, wgt[u], l_all);
+    }
+    const bool result = p.nsplit == 1;
+    const float inv = result ? (l_all > 0.f ? 1.f / l_all : 0.f) : 1.f;
+    float x[CH];
+#pragma unroll
+    for (int c = 0; c < CH; ++c) {
+      x[c] = 0.f;
+#pragma unroll
+      for (int u = 0; u < 4; ++u) x[c] = fmaf(park[u][(c * 4 + wave) * 64 + lane], wgt[u], x[c]);
+      x[c] *= inv;
+    }
+    const int64_t slot = (((int64_t)b * p.T + row[nb]) * p.H + hq[nb]) * p.nsplit + split;
+    const int ch = CH * (4 * g + wave);
+    if (live[nb]) {
+      if (!result || p.out_f32) {
+        float* to = result ? (float*)p.out + b * p.o_sb + hq[nb] * p.o_sh + row[nb] * p.o_st + ch : p.part_o + slot * D + ch;
+#pragma unroll
+        for (int c = 0; c < CH; c += 4) *(float4*)(to + c) = make_float4(x[c], x[c + 1], x[c + 2], x[c + 3]);
+      } else {
+        uint16_t* to = (uint16_t*)p.out + b * p.o_sb + hq[nb] * p.o_sh + row[nb] * p.o_st + ch;
+#pragma unroll
+        for (int c = 0; c < CH; c += 4) *(uint2*)(to + c) = make_uint2(pack_bf16(x[c], x[c + 1]), pack_bf16(x[c + 2], x[c + 3]));
+      }
+      if (wave == 0 && g == 0) {
+        if (!result) *(float2*)(p.part_ml + slot * 2) = make_float2(m_all, l_all);
+        else if (p.lse != nullptr)
+          p.lse[b * p.lse_sb + hq[nb] * p.lse_sh + row[nb] * p.lse_st] = l_all > 0.f ? (m_all + __log2f(l_all)) * kLn2 : -INFINITY;
+      }
+    }
+  }
+}
+
+}  // namespace fl

@@ -1,5 +1,5 @@
 // Marshalling of the PyTorch entry points (attention and its backward pass, with and without the variants' extra tensors, a decode
-// step, a chunk of a paged prefill, rotary positions, weights of cached keys, eviction): torch tensors in, C-ABI descriptors filled, outputs and workspace taken from torch's
+// step, a chunk of a paged prefill, rotary positions, weights of cached keys, eviction, normalised heads, a cache in 4 bits): torch tensors in, C-ABI descriptors filled, outputs and workspace taken from torch's
 // allocator, one call of libflattn.so, the fl_status and the outputs back.  No attention arithmetic and no kernel is here.
 //
 // The same in Python (ctypes structures filled field by field) cost 20 us of a 31 us causal call on [1, 8, 128, 64] and of
@@ -399,6 +399,190 @@ std::tuple<int, Tensor> rotary_append(const Tensor& q, const Tensor& k, const Te
   return {status, qo};
 }
 
+// ---- heads normalised and turned; a cache in 4 bits ----
+
+void check_head_weight(const char* name, const OptTensor& w, const Tensor& q) {
+  if (w.has_value()) check_array(name, w, at::kFloat, {q.size(-1)}, q.device(), true, false);
+}
+fl_head_norm norm_desc(const OptTensor& qw, const OptTensor& kw, double eps) {
+  fl_head_norm n = {};
+  n.struct_size = sizeof(n);
+  n.eps = (float)eps;
+  n.q_weight = ptr<const float>(qw);
+  n.k_weight = ptr<const float>(kw);
+  return n;
+}
+
+// q [B, H, S, D] and k, which may be missing, normalised and turned; the outputs have their layouts
+std::tuple<int, Tensor, OptTensor> norm_rotary(const Tensor& q, const OptTensor& k, const OptTensor& qw, const OptTensor& kw, const Tensor& positions,
+                                               const Tensor& inv_freq, const std::vector<int64_t>& sections, bool interleaved, double eps,
+                                               int64_t stream) {
+  const c10::DeviceGuard guard(q.device());
+  const fl_rotary r = rotary_desc(positions, inv_freq, sections, interleaved, false);
+  const fl_head_norm n = norm_desc(qw, kw, eps);
+  Tensor qo = at::empty_like(q);
+  OptTensor ko;
+  const fl_tensor tq = rows_desc(q);
+  fl_tensor tqo = rows_desc(qo), tk = {}, tko = {};
+  if (k.has_value()) {
+    ko = at::empty_like(*k);
+    tk = rows_desc(*k);
+    tko = rows_desc(*ko);
+  }
+  const int status = fl_norm_rotary(&tq, k.has_value() ? &tk : nullptr, &r, &n, &tqo, k.has_value() ? &tko : nullptr, (void*)stream);
+  return {status, qo, ko};
+}
+
+// ... of a call, with its checks
+std::tuple<int, Tensor, OptTensor> norm_rotary_checked(const Tensor& q, const OptTensor& k, const OptTensor& qw, const OptTensor& kw,
+                                                       const OptTensor& positions, const OptTensor& inv_freq, const Sections& given, bool interleaved,
+                                                       double eps, int64_t stream) {
+  const auto [p, sections] = check_rotary(q, k, positions, inv_freq, given, q.size(0), q.size(2));
+  check_head_weight("q_weight", qw, q);
+  check_head_weight("k_weight", kw, q);
+  return norm_rotary(q, k, qw, kw, p, *inv_freq, sections, interleaved, eps, stream);
+}
+
+// The status and the gradients of q, k, qw, kw, of those that are wanted (1, 2, 4, 8) where a gradient dq or dk has arrived.
+std::tuple<int, std::vector<OptTensor>> norm_gradient(const Tensor& q, const OptTensor& k, const OptTensor& qw, const OptTensor& kw, const OptTensor& dq_in,
+                                                      const OptTensor& dk_in, const Tensor& positions, const Tensor& inv_freq,
+                                                      const std::vector<int64_t>& sections, bool interleaved, double eps, int wanted, int64_t stream) {
+  const c10::DeviceGuard guard(q.device());
+  const fl_rotary r = rotary_desc(positions, inv_freq, sections, interleaved, false);
+  const fl_head_norm n = norm_desc(qw, kw, eps);
+  std::vector<OptTensor> g(4);
+  if (!dq_in.has_value()) wanted &= ~5;
+  if (!dk_in.has_value()) wanted &= ~10;
+  if (wanted == 0) return {0, g};
+  const bool of_q = (wanted & 5) != 0, of_k = (wanted & 10) != 0;
+  Tensor dq, dk;
+  fl_tensor tq = {}, tk = {}, tdq = {}, tdk = {}, tgq = {}, tgk = {};
+  if (of_q) {
+    dq = readable(*dq_in);
+    tq = rows_desc(q);
+    tdq = rows_desc(dq);
+  }
+  if (of_k) {
+    dk = readable(*dk_in);
+    tk = rows_desc(*k);
+    tdk = rows_desc(dk);
+  }
+  if (wanted & 1) g[0] = at::empty_like(q), tgq = rows_desc(*g[0]);
+  if (wanted & 2) g[1] = at::empty_like(*k), tgk = rows_desc(*g[1]);
+  if (wanted & 4) g[2] = at::empty_like(*qw);
+  if (wanted & 8) g[3] = at::empty_like(*kw);
+  Tensor ws;
+  const size_t room = wanted & 12 ? fl_norm_rotary_bwd_workspace_size(of_q ? &tq : nullptr, of_k ? &tk : nullptr, &r) : 0;
+  if (room != 0) ws = bytes(room, q);
+  const int status = fl_norm_rotary_bwd(of_q ? &tq : nullptr, of_k ? &tk : nullptr, of_q ? &tdq : nullptr, of_k ? &tdk : nullptr, &r, &n,
+                                        wanted & 1 ? &tgq : nullptr, wanted & 2 ? &tgk : nullptr, ptr<float>(g[2]), ptr<float>(g[3]),
+                                        room != 0 ? ws.data_ptr() : nullptr, room, (void*)stream);
+  return {status, g};
+}
+
+// The page size of 4-bit caches [pages, Hkv, bytes] whose heads have D channels, and the host-side bound of the lengths, after their checks
+std::tuple<int64_t, int64_t> check_cache_mx4(const Tensor& q, const Tensor& k_cache, const Tensor& v_cache, const OptTensor& seq_lens, const OptTensor& table,
+                                             std::optional<int64_t> max_seq_len) {
+  const int64_t D = q.size(-1), token = D / 2 + D / 32;
+  for (const Tensor* c : {&k_cache, &v_cache})
+    need(c->dim() == 3 && c->scalar_type() == at::kByte && c->device() == q.device() && (c->size(2) <= 1 || c->stride(2) == 1),
+         "the caches must be uint8 tensors [pages, Hkv, bytes] of unit inner stride on ", q.device());
+  need(k_cache.sizes() == v_cache.sizes(), "k_cache and v_cache must have one shape");
+  need(D == 64 || D == 128, "caches in 4 bits take heads of 64 or 128 channels, got ", D);
+  need(k_cache.size(2) > 0 && k_cache.size(2) % (8 * token) == 0, "pages of ", k_cache.size(2), " bytes a head are not whole octets of tokens of ", token, " bytes");
+  const int64_t B = q.size(0), page_size = k_cache.size(2) / token;
+  check_array("seq_lens", seq_lens, at::kInt, {B}, q.device(), true, false);
+  if (table.has_value()) {
+    need(table->dim() == 2, "block_table must be [B, max_pages]");
+    check_array("block_table", table, at::kInt, {B, table->size(1)}, q.device(), false, true);
+  }
+  const int64_t held = (table.has_value() ? table->size(1) : 1) * page_size, n = max_seq_len.value_or(held);
+  need(n >= 0 && n <= INT32_MAX, "max_seq_len = ", n);
+  need(!table.has_value() || n <= held, "max_seq_len = ", n, " is more than the ", table.has_value() ? table->size(1) : 1, " pages of block_table hold");
+  return {page_size, n};
+}
+fl_tensor mx4_desc(const Tensor& t, int64_t page_size, int64_t D) {
+  fl_tensor d = {};
+  d.ptr = t.data_ptr();
+  d.dtype = FL_MX4;
+  const int64_t size[5] = {t.size(0), 1, t.size(1), page_size, D}, stride[5] = {t.stride(0), 0, t.stride(1), 0, 1};
+  for (int a = 0; a < 5; ++a) d.size[a] = size[a], d.stride[a] = stride[a];
+  return d;
+}
+fl_paged_kv paged_mx4(int64_t page_size, const Tensor& seq_lens, const OptTensor& table, int64_t max_seq_len) {
+  fl_paged_kv kv = {};
+  kv.struct_size = sizeof(kv);
+  kv.block_table = ptr<const int32_t>(table);
+  kv.table_stride = table.has_value() ? row_step(*table) : 0;
+  kv.page_size = (int32_t)page_size;
+  kv.seq_lens = (const int32_t*)seq_lens.data_ptr();
+  kv.max_seq_len = (int32_t)max_seq_len;
+  return kv;
+}
+
+// rotary_append() of normalised heads (eps None: of heads as they are), into bf16 or 4-bit caches; what the latter hold of the tokens, if wanted
+std::tuple<int, Tensor, OptTensor, OptTensor> norm_append(const Tensor& q, const Tensor& k, const Tensor& v, const OptTensor& positions,
+                                                          const OptTensor& inv_freq, const Sections& given, bool interleaved, const OptTensor& qw,
+                                                          const OptTensor& kw, std::optional<double> eps, const Tensor& k_cache, const Tensor& v_cache,
+                                                          const OptTensor& seq_lens, const OptTensor& table, std::optional<int64_t> bound, bool want_held,
+                                                          int64_t stream) {
+  const c10::DeviceGuard guard(q.device());
+  const auto [p, sections] = check_rotary(q, k, positions, inv_freq, given, q.size(0), q.dim() == 4 ? q.size(2) : 1);
+  check_head_weight("q_weight", qw, q);
+  check_head_weight("k_weight", kw, q);
+  need(eps.has_value() || (!qw.has_value() && !kw.has_value()), "weights without norms (eps is None)");
+  const bool mx4 = k_cache.scalar_type() == at::kByte;
+  need(mx4 || !want_held, "return_held goes with caches in 4 bits");
+  int64_t page_size = 0, max_seq_len = 0;
+  if (mx4) std::tie(page_size, max_seq_len) = check_cache_mx4(q, k_cache, v_cache, seq_lens, table, bound);
+  else max_seq_len = check_cache(q, k_cache, v_cache, seq_lens, table, bound);
+  need(k.sizes() == v.sizes() && v.scalar_type() == q.scalar_type() && v.device() == q.device() && k.size(1) == k_cache.size(mx4 ? 1 : 2), "k ", k.sizes(),
+       " and v ", v.sizes(), " do not go with the cache ", k_cache.sizes());
+  const fl_rotary r = rotary_desc(p, *inv_freq, sections, interleaved, false);
+  const fl_head_norm n = norm_desc(qw, kw, eps.value_or(0.));
+  Tensor qo = at::empty_like(q);
+  const fl_tensor tq = rows_desc(q), tk = rows_desc(k), tv = rows_desc(v);
+  fl_tensor tqo = rows_desc(qo), tkc = mx4 ? mx4_desc(k_cache, page_size, q.size(-1)) : cache_desc(k_cache),
+            tvc = mx4 ? mx4_desc(v_cache, page_size, q.size(-1)) : cache_desc(v_cache), tkh = {}, tvh = {};
+  OptTensor kh, vh;
+  if (want_held) {
+    kh = at::empty(k.sizes(), k.options());
+    vh = at::empty(v.sizes(), v.options());
+    tkh = rows_desc(*kh);
+    tvh = rows_desc(*vh);
+  }
+  const fl_paged_kv kv = mx4 ? paged_mx4(page_size, *seq_lens, table, max_seq_len) : paged_kv(k_cache, *seq_lens, table, (int)max_seq_len);
+  const int status = fl_norm_rotary_append(&tq, &tk, &tv, &r, eps.has_value() ? &n : nullptr, &kv, &tqo, &tkc, &tvc, want_held ? &tkh : nullptr,
+                                           want_held ? &tvh : nullptr, (void*)stream);
+  return {status, qo, kh, vh};
+}
+
+// A decode step (q [B, H, D] or [B, H, T, D]) or a chunk of rows (q [B, H, Sq, D]) over 4-bit caches
+std::tuple<int, int64_t, Tensor, OptTensor> paged_4bit(bool decode, const Tensor& q, const Tensor& k_cache, const Tensor& v_cache, const OptTensor& lens,
+                                                       const OptTensor& table, std::optional<int64_t> bound, double scale, int mod, double softcap, int mask,
+                                                       int window, const OptTensor& slopes, const OptTensor& workspace, bool want_lse, int64_t stream) {
+  const c10::DeviceGuard guard(q.device());
+  const auto [page_size, max_seq_len] = check_cache_mx4(q, k_cache, v_cache, lens, table, bound);
+  check_slopes(slopes, q);
+  check_workspace(workspace, q);
+  const fl_tensor tq = rows_desc(q), tk = mx4_desc(k_cache, page_size, q.size(-1)), tv = mx4_desc(v_cache, page_size, q.size(-1));
+  Tensor out = at::empty(q.sizes(), q.options());
+  fl_tensor tout = rows_desc(out), tlse = {};
+  OptTensor lse;
+  if (want_lse) {
+    lse = at::empty(q.sizes().slice(0, q.dim() - 1), q.options().dtype(at::kFloat));
+    tlse = q.dim() == 3 ? desc5(*lse, {0, -1, 1, -1, -1}) : desc5(*lse, {0, -1, 1, 2, -1});
+  }
+  const fl_paged_kv kv = paged_mx4(page_size, *lens, table, max_seq_len);
+  const size_t room = std::max<size_t>((decode ? fl_attn_decode_mx4_workspace_size : fl_attn_prefill_mx4_workspace_size)(&tq, &tk, &kv), 16);
+  if (workspace.has_value() && workspace->nbytes() < room) return {0, (int64_t)room, out, lse};
+  const Tensor ws = workspace.has_value() ? *workspace : bytes(room, q);
+  const fl_variant_desc d = variant(scale, mod, softcap, mask, window, 0, 0);
+  const fl_aux a = aux_of(slopes, std::nullopt, std::nullopt, ws);
+  const int status = (decode ? fl_attn_decode_mx4 : fl_attn_prefill_mx4)(&tq, &tk, &tv, &kv, &d, &a, &tout, want_lse ? &tlse : nullptr, (void*)stream);
+  return {status, (int64_t)room, out, lse};
+}
+
 // paged() for a decode step (q [B, H, D] or [B, H, T, D]) that adds up the keys' weights [B, Hkv, C]
 std::tuple<int, int64_t, Tensor, OptTensor> decode_weights(const Tensor& q, const Tensor& k_cache, const Tensor& v_cache, const OptTensor& w,
                                                            const OptTensor& lens, const OptTensor& table, std::optional<int64_t> bound, double scale,
@@ -646,6 +830,71 @@ std::tuple<int, OptTensor, OptTensor> rotary_node(const Tensor& q, const OptTens
   return {0, qo, ko};
 }
 
+// The gradients of norm_rotary(), taken through Function::apply unseen, so that a derivative of them raises instead of counting as zero.
+struct NormGradientNode : torch::autograd::Function<NormGradientNode> {
+  static torch::autograd::variable_list forward(torch::autograd::AutogradContext*, at::TensorList, const std::vector<OptTensor>* done) {
+    torch::autograd::variable_list out;
+    for (const OptTensor& g : *done)
+      if (g.has_value()) out.push_back(*g);
+    return out;
+  }
+  static torch::autograd::variable_list backward(torch::autograd::AutogradContext*, const torch::autograd::variable_list&) {
+    throw std::runtime_error("norm_rotary() has no second derivative");
+  }
+};
+struct NormNode : torch::autograd::Function<NormNode> {
+  static torch::autograd::variable_list forward(torch::autograd::AutogradContext* ctx, const Tensor& q, const OptTensor& k, const OptTensor& qw,
+                                                const OptTensor& kw, const Tensor& positions, const Tensor& inv_freq,
+                                                const std::vector<int64_t>& sections, bool interleaved, double eps, const Turned& done) {
+    ctx->set_materialize_grads(false);
+    auto opt = [](const OptTensor& t) { return t.has_value() ? savable(*t) : Tensor(); };
+    ctx->save_for_backward({savable(q), opt(k), opt(qw), opt(kw), savable(positions), savable(inv_freq)});
+    ctx->saved_data["sections"] = sections;
+    ctx->saved_data["interleaved"] = interleaved;
+    ctx->saved_data["eps"] = eps;
+    torch::autograd::variable_list out = {*done.q};
+    if (done.k.has_value()) out.push_back(*done.k);
+    return out;
+  }
+  static torch::autograd::variable_list backward(torch::autograd::AutogradContext* ctx, const torch::autograd::variable_list& grads) {
+    const auto t = ctx->get_saved_variables();
+    auto opt = [](const Tensor& x) { return x.defined() ? OptTensor(x) : OptTensor(); };
+    int wanted = 0, edge = 0;                      // (the node has an edge for each input that is there)
+    for (int n = 0; n < 4; ++n)
+      if (t[n].defined() && ctx->needs_input_grad(edge++)) wanted |= 1 << n;
+    const OptTensor dq = opt(grads[0]), dk = grads.size() > 1 ? opt(grads[1]) : OptTensor();
+    auto [status, g] = norm_gradient(t[0], opt(t[1]), opt(t[2]), opt(t[3]), dq, dk, t[4], t[5], ctx->saved_data["sections"].toIntVector(),
+                                     ctx->saved_data["interleaved"].toBool(), ctx->saved_data["eps"].toDouble(), wanted, current_stream(t[0]));
+    if (status != 0) throw_status(status);
+    if (at::GradMode::is_enabled()) {
+      torch::autograd::variable_list from = {t[0]};
+      for (const Tensor& x : {t[1], t[2], t[3], grads[0], grads.size() > 1 ? grads[1] : Tensor()})
+        if (x.defined()) from.push_back(x);
+      const auto held = NormGradientNode::apply(at::TensorList(from), (const std::vector<OptTensor>*)&g);
+      size_t n = 0;
+      for (OptTensor& x : g)
+        if (x.has_value()) x = held[n++];
+    }
+    torch::autograd::variable_list out(10);
+    for (int n = 0; n < 4; ++n)
+      if (g[n].has_value()) out[n] = *g[n];
+    return out;
+  }
+};
+
+// norm_rotary_checked with a node
+std::tuple<int, Tensor, OptTensor> norm_rotary_node(const Tensor& q, const OptTensor& k, const OptTensor& qw, const OptTensor& kw, const OptTensor& positions,
+                                                    const OptTensor& inv_freq, const Sections& given, bool interleaved, double eps, int64_t stream) {
+  const auto [p, sections] = check_rotary(q, k, positions, inv_freq, given, q.size(0), q.size(2));
+  check_head_weight("q_weight", qw, q);
+  check_head_weight("k_weight", kw, q);
+  auto [status, qo, ko] = norm_rotary(q, k, qw, kw, p, *inv_freq, sections, interleaved, eps, stream);
+  if (status != 0) return {status, qo, ko};
+  const OptTensor first = qo;
+  const auto t = NormNode::apply(q, k, qw, kw, p, *inv_freq, sections, interleaved, eps, Turned{first, ko});
+  return {0, t[0], ko.has_value() ? OptTensor(t[1]) : ko};
+}
+
 }  // namespace
 
 PYBIND11_MODULE(_fltorch, m) {
@@ -663,6 +912,12 @@ PYBIND11_MODULE(_fltorch, m) {
   m.def("rotary_checked", &rotary_checked, nogil());
   m.def("rotary_node", &rotary_node, nogil());
   m.def("rotary_append", &rotary_append, nogil());
+  m.def("norm_rotary", &norm_rotary, nogil());
+  m.def("norm_rotary_checked", &norm_rotary_checked, nogil());
+  m.def("norm_rotary_node", &norm_rotary_node, nogil());
+  m.def("norm_gradient", &norm_gradient, nogil());
+  m.def("norm_append", &norm_append, nogil());
+  m.def("paged_4bit", &paged_4bit, nogil());
   m.def("decode_weights", &decode_weights, nogil());
   m.def("key_weights", &key_weights, nogil());
   m.def("evict", &evict, nogil());

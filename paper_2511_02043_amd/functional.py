@@ -14,6 +14,9 @@ second stream, differentiable in every tensor input (fl_attn_bwd_ex).
 Around a bounded key/value cache: `rotary()` (positions with several axes, differentiable), `rotary_append()` (the same for new tokens,
 whose keys and values enter the pages), `decode_attention_weights()` and `prefill_key_weights()` (the weight that each cached key
 receives), `evict_cache()` (the keys of most weight move to fresh pages).
+
+Heads normalised and turned in one pass: `norm_rotary()` (differentiable), `norm_rotary_append()` (the same for new tokens, into a bf16 cache or
+into one in 4 bits).  The cache in 4 bits: `mx4_cache()` (its pages), `decode_attention_mx4()` and `paged_prefill_attention_mx4()`.
 """
 from __future__ import annotations
 
@@ -524,3 +527,152 @@ def evict_cache(weights: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Ten
     if status:
         fb.check(status)
     return new_lens, new_weights, kept
+
+
+# ---- heads normalised and turned; a cache in 4 bits ---------------------------------------------------------------------
+
+
+class _NormGradient(torch.autograd.Function):
+    """The gradient of _NormRotary as a node of its own, whose own derivative raises."""
+
+    @staticmethod
+    def forward(q, k, q_weight, k_weight, dq, dk, positions, inv_freq, sections, interleaved, eps, wanted):
+        status, grads = _host().norm_gradient(q, k, q_weight, k_weight, dq, dk, positions, inv_freq, sections, interleaved, eps, wanted, _stream(q))
+        if status:
+            fb.check(status)
+        return tuple(grads)
+
+    @staticmethod
+    def setup_context(ctx, inputs, output):
+        pass
+
+    @staticmethod
+    def backward(ctx, *grads):
+        raise RuntimeError("norm_rotary() has no second derivative")
+
+
+class _NormRotary(torch.autograd.Function):
+    """norm_rotary() where torch.func's grad, traces or torch.compile look into the node.  (No rule for vmap and none for forward-mode derivatives:
+    torch refuses both.)"""
+
+    @staticmethod
+    def forward(q, k, q_weight, k_weight, positions, inv_freq, sections, interleaved, eps):
+        status, qo, ko = _host().norm_rotary(q, k, q_weight, k_weight, positions, inv_freq, sections, interleaved, eps, _stream(q))
+        if status:
+            fb.check(status)
+        return qo, ko
+
+    @staticmethod
+    def setup_context(ctx, inputs, output):
+        *tensors, sections, interleaved, eps = inputs
+        ctx.how = sections, interleaved, eps
+        ctx.set_materialize_grads(False)
+        # autograd keeps no tensors made in inference mode: a copy
+        ctx.save_for_backward(*(t.clone() if t is not None and t.is_inference() else t for t in tensors))
+
+    @staticmethod
+    def backward(ctx, dq, dk):
+        q, k, q_weight, k_weight, positions, inv_freq = ctx.saved_tensors
+        wanted = sum(1 << n for n in range(4) if ctx.needs_input_grad[n])
+        if dq is None and dk is None:
+            return (None,) * 9
+        return _NormGradient.apply(q, k, q_weight, k_weight, dq, dk, positions, inv_freq, *ctx.how, wanted) + (None,) * 5
+
+
+def norm_rotary(q: torch.Tensor, k: Optional[torch.Tensor], positions: torch.Tensor, inv_freq: torch.Tensor, q_weight: Optional[torch.Tensor] = None,
+                k_weight: Optional[torch.Tensor] = None, *, eps: float = 1e-6, sections=None, interleaved: bool = False):
+    """RMS norms of query and key heads, then rotary positions, in one pass (fl_norm_rotary): every row x of D channels becomes
+    weight * x / sqrt(mean(x^2) + eps), whose channel pairs turn as in rotary().
+
+    q [B, H, S, D], k [B, Hkv, S, D] (or None), positions, inv_freq, sections, interleaved and layouts as for rotary(), D up to 1024; q_weight and
+    k_weight float32 [D], shared by the heads (None: ones).  Returns the normalised and turned q and k, in their layouts; differentiable (once)
+    in q, k and both weights, not in inv_freq.  The backward pass reads its inputs again: changed in place before it, they raise there."""
+    if not q.is_cuda or q.dtype not in (torch.bfloat16, torch.float32) or q.dim() != 4:
+        raise ValueError("norm_rotary() takes a bf16 or float32 CUDA q of shape [B, H, S, D] (there is no CPU or fallback path)")
+    if getattr(inv_freq, "requires_grad", False) and _grad_enabled():
+        raise ValueError("inv_freq requires a gradient, and norm_rotary() has none for it: pass inv_freq.detach()")
+    if k is None and k_weight is not None:
+        raise ValueError("k_weight without k")
+    sections = _tuple(sections)
+    node = _node_for((q, k, q_weight, k_weight))
+    if node == _PYTHON_NODE:
+        positions, sections = _check_rotary(q, k, positions, inv_freq, sections, q.shape[0], q.shape[2])
+        for name, w in (("q_weight", q_weight), ("k_weight", k_weight)):
+            _check_aux(name, w, torch.float32, (q.shape[-1],), q.device)
+        return _NormRotary.apply(q, k, q_weight, k_weight, positions, inv_freq, sections, bool(interleaved), float(eps))
+    call = _host().norm_rotary_node if node == _NATIVE_NODE else _host().norm_rotary_checked
+    status, qo, ko = call(q, k, q_weight, k_weight, positions, inv_freq, sections, bool(interleaved), float(eps), _stream(q))
+    if status:
+        fb.check(status)
+    return qo, ko
+
+
+def mx4_cache(pages: int, page_size: int, kv_heads: int, head_dim: int, *, device="cuda"):
+    """The key and the value cache of a 4-bit paged cache: zeros, uint8 [pages, kv_heads, page_size * (head_dim / 2 + head_dim / 32)].
+
+    head_dim 64 or 128; page_size a power of two >= 8 (any multiple of 8 without a block table).  For each page and kv head the
+    codes [page_size, head_dim / 2] (channel 2 i in the low half of byte i, 2 i + 1 in the high half; a sign and one of 0, 0.5, 1, 1.5, 2, 3, 4, 6), then the
+    scale bytes [head_dim / 32, page_size]: E stands for 2^(E - 127) and belongs to 32 channels of a token.  68 bytes a token and head of 128
+    channels, of 256 in bf16."""
+    if head_dim not in (64, 128):
+        raise ValueError(f"a cache in 4 bits takes heads of 64 or 128 channels, got {head_dim}")
+    if page_size < 8 or page_size % 8 != 0:
+        raise ValueError(f"page_size must be a multiple of 8, got {page_size}")
+    shape = (pages, kv_heads, page_size * (head_dim // 2 + head_dim // 32))
+    return tuple(torch.zeros(shape, dtype=torch.uint8, device=device) for _ in range(2))
+
+
+def norm_rotary_append(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, positions: torch.Tensor, inv_freq: torch.Tensor, k_cache: torch.Tensor,
+                       v_cache: torch.Tensor, seq_lens: torch.Tensor, block_table: Optional[torch.Tensor] = None,
+                       q_weight: Optional[torch.Tensor] = None, k_weight: Optional[torch.Tensor] = None, *, eps: Optional[float] = 1e-6,
+                       max_seq_len: Optional[int] = None, sections=None, interleaved: bool = False, return_held: bool = False):
+    """norm_rotary() for the newest T tokens of every sequence in serving (fl_norm_rotary_append): returns the normalised and turned q; the normalised and
+    turned keys and the values enter the paged cache at slots seq_lens - T .. seq_lens - 1.
+
+    q [B, H, T, D] with k, v [B, Hkv, T, D], or without the T axis for one token; bf16.  q_weight, k_weight float32 [D] or None; eps None: no norms,
+    turns alone.  Caches: bf16 as for rotary_append(), or the two of mx4_cache(), which hold each value in 4 bits with a scale for 32 channels
+    (a key is rounded from its exact value; infinities are held as the largest finite value, NaN as zero).  positions, seq_lens,
+    block_table, max_seq_len and what is passed over as for rotary_append().  return_held (4-bit caches): also k and v [B, Hkv, (T,) D] bf16 as the
+    cache holds them, e.g. for attention() among the rows of a prompt that nothing is cached before.  Not differentiable."""
+    if not q.is_cuda or q.dtype != torch.bfloat16 or q.dim() not in (3, 4):
+        raise ValueError("norm_rotary_append() takes a bf16 CUDA q of shape [B, H, T, D] or [B, H, D]")
+    status, out, k_held, v_held = _host().norm_append(q, k, v, positions, inv_freq, _tuple(sections), bool(interleaved), q_weight, k_weight, eps, k_cache,
+                                                      v_cache, seq_lens, block_table, max_seq_len, bool(return_held), _stream(q))
+    if status:
+        fb.check(status)
+    return (out, k_held, v_held) if return_held else out
+
+
+def _mx4_call(decode, q, k_cache, v_cache, seq_lens, block_table, max_seq_len, scale, window, softcap, alibi_slopes, workspace, return_lse):
+    status, need, out, lse = _host().paged_4bit(decode, q, k_cache, v_cache, seq_lens, block_table, max_seq_len,
+                                                *_paged_variant(q, scale, window, softcap, alibi_slopes), workspace, return_lse, _stream(q))
+    if status:
+        fb.check(status)
+    _check_workspace(workspace, need)
+    return (out, lse) if return_lse else out
+
+
+def decode_attention_mx4(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor, seq_lens: torch.Tensor,
+                         block_table: Optional[torch.Tensor] = None, *, max_seq_len: Optional[int] = None, scale: Optional[float] = None,
+                         window: Optional[int] = None, softcap: Optional[float] = None, alibi_slopes: Optional[torch.Tensor] = None,
+                         workspace: Optional[torch.Tensor] = None, return_lse: bool = False):
+    """decode_attention() over the two caches of mx4_cache() (fl_attn_decode_mx4): the newest rows of every sequence against its cached keys.
+
+    q [B, H, D] (the newest token) or [B, H, T, D] (the newest T, T * H / Hkv <= 64), bf16, D 64 or 128.  Lengths, block_table, max_seq_len,
+    variants, workspace and results as for decode_attention().  Not differentiable."""
+    if not q.is_cuda or q.dtype != torch.bfloat16 or q.dim() not in (3, 4):
+        raise ValueError("decode_attention_mx4() takes a bf16 CUDA q of shape [B, H, D] or [B, H, T, D]")
+    return _mx4_call(True, q, k_cache, v_cache, seq_lens, block_table, max_seq_len, scale, window, softcap, alibi_slopes, workspace, return_lse)
+
+
+def paged_prefill_attention_mx4(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor, seq_lens: torch.Tensor,
+                                block_table: Optional[torch.Tensor] = None, *, max_seq_len: Optional[int] = None, scale: Optional[float] = None,
+                                window: Optional[int] = None, softcap: Optional[float] = None, alibi_slopes: Optional[torch.Tensor] = None,
+                                workspace: Optional[torch.Tensor] = None, return_lse: bool = False):
+    """paged_prefill_attention() over the two caches of mx4_cache() (fl_attn_prefill_mx4): the last Sq tokens of every sequence, already cached, attend
+    causally to its cached keys.
+
+    q [B, H, Sq, D] bf16, D 64 or 128; the rest as for paged_prefill_attention().  Not differentiable."""
+    if not q.is_cuda or q.dtype != torch.bfloat16 or q.dim() != 4:
+        raise ValueError("paged_prefill_attention_mx4() takes a bf16 CUDA q of shape [B, H, Sq, D]")
+    return _mx4_call(False, q, k_cache, v_cache, seq_lens, block_table, max_seq_len, scale, window, softcap, alibi_slopes, workspace, return_lse)
