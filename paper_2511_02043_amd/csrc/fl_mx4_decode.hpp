@@ -69,8 +69,11 @@ __device__ __forceinline__ float quarter_sum(float x) {
 //     is what the second contraction wants of P: no exchange between lanes;
 //   * for that one, a lane has keys 8 g .. + 7 of channels D/16 m .. + D/16 - 1: the codes of two keys are converted two channels at a time, then
 //     paired key by key.
+// waves of a SIMD: what the registers of an instance leave room for
+constexpr int mx4_decode_waves(int D, int NB) { return NB == 1 ? (D == 128 ? 3 : 4) : (NB == 2 ? 2 : 1); }
+
 template <int D, int MOD, int NB>
-__global__ void __launch_bounds__(256) mx4_decode_kernel(const Mx4DecodeParams p) {
+__global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(mx4_decode_waves(D, NB), mx4_decode_waves(D, NB)))) mx4_decode_kernel(const Mx4DecodeParams p) {
   constexpr int KS = D / 32;                       // steps of the first contraction
   constexpr int CH = D / 16;                       // channels of a lane in the second
   __shared__ float park[4][CH * 4 * 64];
@@ -116,53 +119,63 @@ __global__ void __launch_bounds__(256) mx4_decode_kernel(const Mx4DecodeParams p
   const float c_scale = p.scale * kLog2e;
   const int64_t codes_bytes = (int64_t)p.cache.page_size * (D / 2);
 
-  for (int t = t_begin + wave; t < t_end; t += 4) {
-    // the pages of this lane's eight keys in either contraction (an octet lies in one page; behind the sequence: its last one)
-    const uint8_t *kp, *vp;
-    int k_in, v_in;
-    auto octet = [&](int o, const uint8_t* base, int64_t sp, int64_t sh, int& within) __attribute__((always_inline)) {
-      const int j = min(t * 32 + 8 * o, (len - 1) & ~7);
-      int64_t page = b;
-      within = j;
-      if (p.block_table != nullptr) {
-        page = min(max(p.block_table[(int64_t)b * p.table_stride + (j >> p.page_shift)], 0), p.num_pages - 1);
-        within = j & ((1 << p.page_shift) - 1);
-      }
-      return base + page * sp + hk * sh;
-    };
-    kp = octet(m >> 2, p.cache.k, p.cache.k_sp, p.cache.k_sh, k_in);
-    vp = octet(g, p.cache.v, p.cache.v_sp, p.cache.v_sh, v_in);
-    uint32_t kc[2][KS], vc[8];
-    int ke[2];
+  // A lane's page of its eight keys of tile t in either contraction (an octet lies in one page; behind the sequence: its last one).  The entries of a
+  // tile are requested two tiles ahead of its products, its codes and scales one tile ahead.  The tile behind a wave's last is the last again: a load
+  // that is not there on one path would make the compiler wait for every load on the other.
+  const int t_last = t_begin + wave + max(0, t_end - 1 - t_begin - wave) / 4 * 4;
+  const int32_t* const table = p.block_table + (p.block_table != nullptr ? (int64_t)b * p.table_stride : 0);
+  const int in_page = p.block_table != nullptr ? (1 << p.page_shift) - 1 : -1;
+  struct Pages {
+    int k, v;
+  };
+  auto octet = [&](int t, int o) __attribute__((always_inline)) { return min(min(t, t_last) * 32 + 8 * o, (len - 1) & ~7); };
+  auto lookup = [&](int t) __attribute__((always_inline)) -> Pages {
+    if (p.block_table == nullptr) return {b, b};
+    return {table[octet(t, m >> 2) >> p.page_shift], table[octet(t, g) >> p.page_shift]};
+  };
+  struct Tile {
+    uint32_t k[2][KS], v[8];
+    uint2 ke, ve;                                  // scales of eight keys of the lane's block
+  };
+  const uint8_t* const k_lane = p.cache.k + hk * p.cache.k_sh + (m & 3) * (D / 2) + g * (D / 8);
+  const uint8_t* const v_lane = p.cache.v + hk * p.cache.v_sh + m * (CH / 2);
+  const uint8_t* const ke_lane = p.cache.k + hk * p.cache.k_sh + codes_bytes + (int64_t)(g * (D / 4) / 32) * p.cache.page_size;
+  const uint8_t* const ve_lane = p.cache.v + hk * p.cache.v_sh + codes_bytes + (int64_t)(m * CH / 32) * p.cache.page_size;
+  auto load = [&](int t, const Pages& pages, Tile& x) __attribute__((always_inline)) {
+    const int last = p.num_pages - 1;
+    const int64_t k_page = min(max(pages.k, 0), last) * p.cache.k_sp, v_page = min(max(pages.v, 0), last) * p.cache.v_sp;
+    const int k_in = octet(t, m >> 2) & in_page, v_in = octet(t, g) & in_page;
+    const uint8_t* kp = k_lane + k_page + (int64_t)k_in * (D / 2);
+    const uint8_t* vp = v_lane + v_page + (int64_t)v_in * (D / 2);
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
-      const int j = k_in + 4 * u + (m & 3);
       if constexpr (D == 128) {
-        const uint4 x = *(const uint4*)(kp + (int64_t)j * (D / 2) + g * (D / 8));
-        kc[u][0] = x.x; kc[u][1] = x.y; kc[u][2] = x.z; kc[u][3] = x.w;
+        const uint4 y = *(const uint4*)(kp + 4 * u * (D / 2));
+        x.k[u][0] = y.x; x.k[u][1] = y.y; x.k[u][2] = y.z; x.k[u][3] = y.w;
       } else {
-        const uint2 x = *(const uint2*)(kp + (int64_t)j * (D / 2) + g * (D / 8));
-        kc[u][0] = x.x; kc[u][1] = x.y;
+        const uint2 y = *(const uint2*)(kp + 4 * u * (D / 2));
+        x.k[u][0] = y.x; x.k[u][1] = y.y;
       }
-      ke[u] = kp[codes_bytes + (int64_t)(g * (D / 4) / 32) * p.cache.page_size + j];
     }
+    x.ke = *(const uint2*)(ke_lane + k_page + k_in);
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-      const uint8_t* at = vp + (int64_t)(v_in + i) * (D / 2) + m * (CH / 2);
-      if constexpr (D == 128) vc[i] = *(const uint32_t*)at;
-      else vc[i] = *(const uint16_t*)at;
+      if constexpr (D == 128) x.v[i] = *(const uint32_t*)(vp + i * (D / 2));
+      else x.v[i] = *(const uint16_t*)(vp + i * (D / 2));
     }
-    uint2 ve = *(const uint2*)(vp + codes_bytes + (int64_t)(m * CH / 32) * p.cache.page_size + v_in);
+    x.ve = *(const uint2*)(ve_lane + v_page + v_in);
+  };
 
+  auto compute = [&](int t, const Tile& tile) __attribute__((always_inline)) {
     f32x4 s[NB][2];
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
 #pragma unroll
       for (int nb = 0; nb < NB; ++nb) s[nb][u] = (f32x4){0.f, 0.f, 0.f, 0.f};
-      const float scale = mx4_scale_value(ke[u]);
+      const float scale = mx4_scale_value(((u ? tile.ke.y : tile.ke.x) >> (8 * (m & 3))) & 255);
 #pragma unroll
       for (int f = 0; f < KS; ++f) {
-        const bf16x8 a = __builtin_bit_cast(bf16x8, mx4_bf16x8(kc[u][f], scale));
+        const bf16x8 a = __builtin_bit_cast(bf16x8, mx4_bf16x8(tile.k[u][f], scale));
 #pragma unroll
         for (int nb = 0; nb < NB; ++nb) s[nb][u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, qf[nb][f], s[nb][u], 0, 0, 0);
       }
@@ -172,25 +185,27 @@ __global__ void __launch_bounds__(256) mx4_decode_kernel(const Mx4DecodeParams p
     bf16x8 pf[NB];
 #pragma unroll
     for (int nb = 0; nb < NB; ++nb) {
-      const int lo_key = p.window >= 0 ? pos[nb] - p.window : 0;
-      float x[8], mx = -INFINITY;
+      float x[8], mx = -INFINITY;                  // x: in the log2 domain, but for the plain scores their factor c_scale
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        const int j = jb + i;
         const float raw = s[nb][i >> 2][i & 3];
-        float a;
         if constexpr (MOD == kModSoftcap) {
           const float e = fast_exp2(raw * (2.f * c_scale / p.softcap));
-          a = fmaf(fast_rcp(e + 1.f), -2.f * p.softcap * kLog2e, p.softcap * kLog2e);
+          x[i] = fmaf(fast_rcp(e + 1.f), -2.f * p.softcap * kLog2e, p.softcap * kLog2e);
         } else if constexpr (MOD == kModAlibi) {
-          a = fmaf(raw, c_scale, -slope2[nb] * (float)(pos[nb] - j));
+          x[i] = fmaf(raw, c_scale, -slope2[nb] * (float)(pos[nb] - jb - i));
         } else {
-          a = raw * c_scale;
+          x[i] = raw;
         }
-        if (partial && (j > pos[nb] || j < lo_key)) a = -INFINITY;
-        x[i] = a;
-        mx = fmaxf(mx, a);
       }
+      if (partial) {
+        const int lo_key = p.window >= 0 ? pos[nb] - p.window : 0;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[i] = jb + i > pos[nb] || jb + i < lo_key ? -INFINITY : x[i];
+      }
+#pragma unroll
+      for (int i = 0; i < 8; ++i) mx = fmaxf(mx, x[i]);
+      if constexpr (MOD == kModNone) mx *= c_scale;                                // (a positive factor)
       // as in the step over bf16 pages the running maximum moves only where a score exceeds it by 2^8, here before any lane has
       // looked at the column's others
       if (__builtin_amdgcn_ballot_w64(mx - m_run[nb] > kLazyMaxLog2) != 0) {
@@ -209,7 +224,8 @@ __global__ void __launch_bounds__(256) mx4_decode_kernel(const Mx4DecodeParams p
       uint32_t pw[4];
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        const float p0 = fast_exp2(x[2 * i] - m_safe), p1 = fast_exp2(x[2 * i + 1] - m_safe);
+        const float p0 = fast_exp2(MOD == kModNone ? fmaf(x[2 * i], c_scale, -m_safe) : x[2 * i] - m_safe);
+        const float p1 = fast_exp2(MOD == kModNone ? fmaf(x[2 * i + 1], c_scale, -m_safe) : x[2 * i + 1] - m_safe);
         psum += p0 + p1;
         pw[i] = pack_bf16(p0, p1);
       }
@@ -218,10 +234,11 @@ __global__ void __launch_bounds__(256) mx4_decode_kernel(const Mx4DecodeParams p
     }
     float vs[8];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const int e = ((i < 4 ? ve.x : ve.y) >> (8 * (i & 3))) & 255;
+    for (int i = 0; i < 8; ++i) vs[i] = mx4_scale_value(((i < 4 ? tile.ve.x : tile.ve.y) >> (8 * (i & 3))) & 255);
+    if (t * 32 + 32 > len) {
       // what lies behind the sequence's end in its last page is any bytes: finite, for P is zero there
-      vs[i] = t * 32 + 8 * g + i < len ? mx4_scale_value(e) : 1.f;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) vs[i] = jb + i < len ? vs[i] : 1.f;
     }
 #pragma unroll
     for (int f = 0; f < CH / 2; ++f) {
@@ -229,10 +246,10 @@ __global__ void __launch_bounds__(256) mx4_decode_kernel(const Mx4DecodeParams p
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
         bf16x2 y;
-        if (f == 0) y = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(vc[i], vs[i], 0);
-        else if (f == 1) y = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(vc[i], vs[i], 1);
-        else if (f == 2) y = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(vc[i], vs[i], 2);
-        else y = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(vc[i], vs[i], 3);
+        if (f == 0) y = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(tile.v[i], vs[i], 0);
+        else if (f == 1) y = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(tile.v[i], vs[i], 1);
+        else if (f == 2) y = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(tile.v[i], vs[i], 2);
+        else y = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(tile.v[i], vs[i], 3);
         c[i] = __builtin_bit_cast(uint32_t, y);
       }
       i32x4 lo, hi;
@@ -246,6 +263,24 @@ __global__ void __launch_bounds__(256) mx4_decode_kernel(const Mx4DecodeParams p
         oacc[nb][2 * f] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, lo), pf[nb], oacc[nb][2 * f], 0, 0, 0);
         oacc[nb][2 * f + 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, hi), pf[nb], oacc[nb][2 * f + 1], 0, 0, 0);
       }
+    }
+  };
+
+  int t = t_begin + wave;
+  if (t < t_end) {
+    Tile even, odd;
+    Pages ahead = lookup(t);
+    load(t, ahead, even);
+    ahead = lookup(t + 4);
+    while (true) {
+      load(t + 4, ahead, odd);
+      ahead = lookup(t + 8);
+      compute(t, even);
+      if ((t += 4) >= t_end) break;
+      load(t + 4, ahead, even);
+      ahead = lookup(t + 8);
+      compute(t, odd);
+      if ((t += 4) >= t_end) break;
     }
   }
 
