@@ -612,7 +612,7 @@ const char* fl_last_error_detail(void);
  * the K / V rings in LDS: 2 = a workgroup barrier per key tile, 4 = one per two tiles),
  * "order" (1 = plain, 2 = XCD-aware workgroup order), "pair" (1 = one q-tile per workgroup,
  * 2 = a long and a short q-tile per workgroup), "decode_splits" (key-range splits per sequence and
- * kv head of fl_attn_decode), "bwd_wg_target" (workgroups up to which fl_attn_bwd cuts a group of
+ * kv head of fl_attn_decode and fl_attn_decode_mx4), "bwd_wg_target" (workgroups up to which fl_attn_bwd cuts a group of
  * query heads into subsets; both change the workspace size the matching *_workspace_size reports),
  * "prefill_gather" (fl_attn_prefill_paged: 1 = always copy the pages first, 2 = always read them in place with the
  * forward kernel; either also keeps chunks of a few rows away from the decode kernels), "prefill_pack" (1 = never

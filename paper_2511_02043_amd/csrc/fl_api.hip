@@ -2613,3 +2613,5 @@ fl_status fl::host::forward_of_lengths(const fl_tensor* q, const fl_tensor* k, c
                                        fl_tensor* out, fl_tensor* lse, void* stream, const int32_t* kv_lens) {
   return forward_call(q, k, v, desc, aux, out, lse, stream, kv_lens);
 }
+
+int fl::host::tuned_decode_splits() { return g_tuning.decode_splits; }

@@ -234,6 +234,7 @@ inline fl_status check_cache_mx4(const fl_paged_kv* kv, const fl_tensor* k_cache
       if (t->stride[a] < bytes) return fail(FL_ERR_STRIDE, "%s stride[%d] = %lld is less than a page and head's %lld bytes", name, a, (long long)t->stride[a], (long long)bytes);
       if (t->stride[a] % 16 != 0) return fail(FL_ERR_ALIGN, "%s stride[%d] not a multiple of 16 bytes", name, a);
     }
+    if (pages > 1 && t->stride[0] >= (1LL << 32)) return fail(FL_ERR_STRIDE, "%s page stride is not below 2^32 bytes", name);
     if (rows_overlap(Hkv, t->stride[2], pages, t->stride[0], bytes)) return fail(FL_ERR_STRIDE, "%s strides: pages overlap", name);
   }
   return FL_OK;
@@ -242,6 +243,9 @@ inline fl_status check_cache_mx4(const fl_paged_kv* kv, const fl_tensor* k_cache
 // The forward pass behind fl_attn_fwd on keys and values [B, 1, Hkv, L, D] of which sequence b has kv_lens[b] (device): its query rows are the last of those.
 fl_status forward_of_lengths(const fl_tensor* q, const fl_tensor* k, const fl_tensor* v, const fl_variant_desc* desc, const fl_aux* aux, fl_tensor* out,
                              fl_tensor* lse, void* stream, const int32_t* kv_lens);
+
+// What fl_set_tuning("decode_splits") asks for in this thread; 0: nothing.
+int tuned_decode_splits();
 
 }  // namespace host
 }  // namespace fl

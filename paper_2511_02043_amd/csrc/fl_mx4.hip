@@ -3,6 +3,7 @@
 #include <algorithm>
 #include <cstring>
 
+#include "fl_bwd_registry.hpp"
 #include "fl_host.hpp"
 #include "fl_mx4_decode.hpp"
 
@@ -15,18 +16,23 @@ constexpr int64_t kMostPairs = 64;                 // (query row, head) pairs of
 // Splits of a sequence's keys, from the shapes and the host-side bound of the lengths alone.
 int splits_of(int64_t B, int64_t Hkv, int64_t max_seq_len) {
   const int64_t tiles = (max_seq_len + 31) / 32, units = std::max<int64_t>(1, B * Hkv);
-  const int64_t want = std::min<int64_t>({(1024 + units - 1) / units, tiles / 4, 64});
+  if (tuned_decode_splits() > 0) return (int)std::max<int64_t>(1, std::min<int64_t>(tuned_decode_splits(), tiles));
+  const int64_t want = std::min<int64_t>({(512 + units - 1) / units, tiles / 4, 64});
   return (int)std::max<int64_t>(1, want);
 }
 
 size_t decode_bytes(int64_t B, int64_t T, int64_t H, int64_t D, int ns) { return (size_t)(B * T * H * ns) * (size_t)(D + 2) * sizeof(float); }
 
+template <int D, int MOD, int NB>
+hipError_t launch_blocks(const fl::Mx4DecodeParams& p, int blocks, hipStream_t stream) {
+  const hipError_t e = fl::raise_lds_limit(fl::mx4_decode_kernel<D, MOD, NB>);
+  if (e != hipSuccess) return e;
+  hipLaunchKernelGGL((fl::mx4_decode_kernel<D, MOD, NB>), dim3(blocks), dim3(256), (fl::Mx4Ring<D, NB>::LDS), stream, p);
+  return hipGetLastError();
+}
 template <int D, int MOD>
 hipError_t launch_decode(const fl::Mx4DecodeParams& p, int blocks, int pairs, hipStream_t stream) {
-  if (pairs <= 16) hipLaunchKernelGGL((fl::mx4_decode_kernel<D, MOD, 1>), dim3(blocks), dim3(256), 0, stream, p);
-  else if (pairs <= 32) hipLaunchKernelGGL((fl::mx4_decode_kernel<D, MOD, 2>), dim3(blocks), dim3(256), 0, stream, p);
-  else hipLaunchKernelGGL((fl::mx4_decode_kernel<D, MOD, 4>), dim3(blocks), dim3(256), 0, stream, p);
-  return hipGetLastError();
+  return pairs <= 16 ? launch_blocks<D, MOD, 1>(p, blocks, stream) : (pairs <= 32 ? launch_blocks<D, MOD, 2>(p, blocks, stream) : launch_blocks<D, MOD, 4>(p, blocks, stream));
 }
 template <int D>
 hipError_t launch_decode(uint32_t mod, const fl::Mx4DecodeParams& p, int blocks, int pairs, hipStream_t stream) {
@@ -185,8 +191,8 @@ fl_status fl_attn_prefill_mx4(const fl_tensor* q, const fl_tensor* k_cache, cons
   if (!fl_variant_supported(&inner, FL_BF16, (int)D, (int)D)) return fail(FL_ERR_UNSUPPORTED, "no forward kernel for D=%lld score_mod=%u with this mask", (long long)D, desc->score_mod);
   const size_t half = dense_bytes(B, Hkv, D, L);
   if ((st = check_workspace(aux, 2 * half)) != FL_OK) return st;
-  const int64_t total = B * Hkv * L * (D / 32);
-  if ((total + 255) / 256 > 0x7fffffffLL) return fail(FL_ERR_SHAPE, "too many rows to unpack");
+  const int64_t per_head = (L + fl::kUnpackKeys - 1) / fl::kUnpackKeys, blocks = B * Hkv * 2 * per_head;
+  if (blocks > 0x7fffffffLL) return fail(FL_ERR_SHAPE, "too many rows to unpack");
   fl_tensor kd, vd;
   memset(&kd, 0, sizeof(kd));
   kd.dtype = FL_BF16;
@@ -195,7 +201,7 @@ fl_status fl_attn_prefill_mx4(const fl_tensor* q, const fl_tensor* k_cache, cons
   vd = kd;
   kd.ptr = aux->workspace;
   vd.ptr = (char*)aux->workspace + half;
-  if (total > 0) {
+  if (blocks > 0) {
     fl::Mx4UnpackParams u;
     memset(&u, 0, sizeof(u));
     u.cache = cache_of(k_cache, v_cache, kv);
@@ -207,12 +213,12 @@ fl_status fl_attn_prefill_mx4(const fl_tensor* q, const fl_tensor* k_cache, cons
     u.page_shift = page_shift;
     u.num_pages = (int)k_cache->size[0];
     u.max_len = kv->max_seq_len;
-    u.Hkv = (int)Hkv;
     u.L = (int)L;
-    u.D = (int)D;
-    u.blocks = (int)(D / 32);
-    u.total = total;
-    hipLaunchKernelGGL(fl::mx4_unpack_kernel, dim3((unsigned)((total + 255) / 256), 2), dim3(256), 0, stream, u);
+    u.by_blocks = fl::Divisor::of(per_head);
+    u.by_heads = fl::Divisor::of(2);
+    u.by_hkv = fl::Divisor::of(Hkv);
+    if (D == 128) hipLaunchKernelGGL(fl::mx4_unpack_kernel<128>, dim3((unsigned)blocks), dim3(256), 0, stream, u);
+    else hipLaunchKernelGGL(fl::mx4_unpack_kernel<64>, dim3((unsigned)blocks), dim3(256), 0, stream, u);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return fail(FL_ERR_LAUNCH, "unpack launch: %s", hipGetErrorString(e));
   }

@@ -6,43 +6,54 @@
 namespace fl {
 
 typedef __attribute__((ext_vector_type(4))) float f32x4;
+typedef __attribute__((ext_vector_type(2))) int i32x2;
 
 // Every sequence's cached rows as dense bf16 tensors [B, Hkv, L, D], row j token j, for the forward kernel that a long chunk of queries runs through.
-// Rows from a sequence's length on are left as they are: that kernel is told the length.  A thread has a block of 32 channels of a key or
-// a value (blockIdx.y): 17 bytes in, 64 out.
+// Rows from a sequence's length on are left as they are: that kernel is told the length.  A workgroup has 128 keys, or values, of a kv head; a thread has
+// eight channels of every 16th (D = 64: 32nd) of them, all requested before the first is converted, so that a wave stores runs of 1 KB.
+constexpr int kUnpackKeys = 128;
 struct Mx4UnpackParams {
   Mx4Cache cache;
   uint16_t* dst[2];
   const int32_t* block_table;
   const int32_t* seq_lens;
-  int32_t table_stride, page_shift, num_pages, max_len, Hkv, L, D, blocks;           // blocks = D / 32
-  int64_t total;                                                                     // B * Hkv * L * blocks
+  int32_t table_stride, page_shift, num_pages, max_len, L;
+  Divisor by_blocks, by_heads, by_hkv;             // workgroups of a kv head, 2, Hkv
 };
+template <int D>
 __global__ void __launch_bounds__(256) mx4_unpack_kernel(const Mx4UnpackParams p) {
-  const int64_t idx = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  if (idx >= p.total) return;
-  const int blk = (int)(idx % p.blocks);
-  int64_t rest = idx / p.blocks;
-  const int j = (int)(rest % p.L);
-  rest /= p.L;
-  const int hk = (int)(rest % p.Hkv), b = (int)(rest / p.Hkv);
-  const int len = min(max(p.seq_lens[b], 0), p.max_len);
-  if (j >= len) return;
-  int64_t page = b;
-  int within = j;
-  if (p.block_table != nullptr) {
-    page = min(max(p.block_table[(int64_t)b * p.table_stride + (j >> p.page_shift)], 0), p.num_pages - 1);
-    within = j & ((1 << p.page_shift) - 1);
+  constexpr int LANES = D / 8, ROWS = 256 / LANES, N = kUnpackKeys / ROWS;
+  int rest, blk, which, bhk, b, hk;
+  p.by_blocks.split(blockIdx.x, rest, blk);
+  p.by_heads.split(rest, bhk, which);
+  p.by_hkv.split(bhk, b, hk);
+  const int len = min(max(p.seq_lens[b], 0), p.max_len), c = threadIdx.x % LANES, j0 = blk * kUnpackKeys + threadIdx.x / LANES;
+  if (blk * kUnpackKeys >= len) return;
+  const uint8_t* base = which ? p.cache.v + hk * p.cache.v_sh : p.cache.k + hk * p.cache.k_sh;
+  const int64_t sp = which ? p.cache.v_sp : p.cache.k_sp, scales = (int64_t)p.cache.page_size * (D / 2) + (int64_t)(c / 4) * p.cache.page_size;
+  int page[N], within[N];
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    const int j = min(j0 + i * ROWS, len - 1);     // (past the end: the last key again, not stored)
+    page[i] = b;
+    within[i] = j;
+    if (p.block_table != nullptr) {
+      page[i] = p.block_table[(int64_t)b * p.table_stride + (j >> p.page_shift)];
+      within[i] = j & ((1 << p.page_shift) - 1);
+    }
   }
-  const bool values = blockIdx.y != 0;
-  const uint8_t* at = values ? p.cache.v + page * p.cache.v_sp + hk * p.cache.v_sh : p.cache.k + page * p.cache.k_sp + hk * p.cache.k_sh;
-  const uint4 codes = *(const uint4*)(at + (int64_t)within * (p.D / 2) + blk * 16);
-  const float scale = mx4_scale_value(at[(int64_t)p.cache.page_size * (p.D / 2) + (int64_t)blk * p.cache.page_size + within]);
-  uint4* to = (uint4*)(p.dst[values ? 1 : 0] + idx * 32);
-  to[0] = mx4_bf16x8(codes.x, scale);
-  to[1] = mx4_bf16x8(codes.y, scale);
-  to[2] = mx4_bf16x8(codes.z, scale);
-  to[3] = mx4_bf16x8(codes.w, scale);
+  uint32_t codes[N];
+  int e[N];
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    const uint8_t* at = base + min(max(page[i], 0), p.num_pages - 1) * sp;
+    codes[i] = *(const uint32_t*)(at + (int64_t)within[i] * (D / 2) + c * 4);
+    e[i] = at[scales + within[i]];
+  }
+  uint16_t* to = p.dst[which] + ((int64_t)bhk * p.L + j0) * D + c * 8;
+#pragma unroll
+  for (int i = 0; i < N; ++i)
+    if (j0 + i * ROWS < len) *(uint4*)(to + (int64_t)i * ROWS * D) = mx4_bf16x8(codes[i], mx4_scale_value(e[i]));
 }
 
 // ---- the decode step over a cache in 4 bits ----
@@ -61,46 +72,57 @@ __device__ __forceinline__ float quarter_sum(float x) {
   return x + __shfl_xor(x, 32);
 }
 
-// A workgroup owns one (sequence, kv head, split of the key range); its four waves take tiles of 32 keys in turn.  NB blocks of 16
-// (query row, head) pairs are the columns of the matrix products, S^T = K Q^T and O^T += V^T P^T on 16 x 16 x 32 instructions:
+// A workgroup owns one (sequence, kv head, split of the key range), a wave a run of its tiles of 32 keys.  NB blocks of 16 (query row, head) pairs are the columns of the matrix products, S^T = K Q^T and O^T += V^T P^T on 16 x 16 x 32 instructions:
 //   * lane = (g, m), g = lane / 16.  The order of a contraction's terms is free, so that a lane's codes of one key are a quarter of its row in
 //     one load, channels D/4 g + 8 s + .. in step s, and its block's scale goes into the conversion;
 //   * row m of product u = 0, 1 is key 8 (m / 4) + 4 u + m % 4 of the tile.  A lane's scores are then those of keys 8 g .. 8 g + 7 in order, which
 //     is what the second contraction wants of P: no exchange between lanes;
 //   * for that one, a lane has keys 8 g .. + 7 of channels D/16 m .. + D/16 - 1: the codes of two keys are converted two channels at a time, then
 //     paired key by key.
-// waves of a SIMD: what the registers of an instance leave room for
-constexpr int mx4_decode_waves(int D, int NB) { return NB == 1 ? (D == 128 ? 3 : 4) : (NB == 2 ? 2 : 1); }
+// Waves of a SIMD, which are workgroups of a compute unit: what the registers of an instance leave room for.  LDS is shared out among them as rings.
+constexpr int mx4_decode_waves(int D, int NB) { return NB == 1 ? 4 : (NB == 2 ? 2 : 1); }
+template <int D, int NB>
+struct Mx4Ring {
+  static constexpr int V = 32 * (D / 2), E = 2 * V, STAGE = E + 256;             // bytes: keys, values, scales
+  static constexpr int LOADS = D == 128 ? 5 : 3;                                 // of a tile
+  static constexpr int ROOM = 160 * 1024 / (4 * mx4_decode_waves(D, NB)) / 16 * 16 - 512;
+  static constexpr int STAGES = ROOM / STAGE < 8 ? ROOM / STAGE : 8;
+  static constexpr int ENTRIES = STAGES * STAGE, BYTES = ENTRIES + 512, LDS = 4 * BYTES;
+  static_assert(STAGES >= 2 && (STAGES - 1) * LOADS < 64 && 16 - STAGES >= STAGES, "a wave's ring");
+  static_assert((D / 16 * 4 * 64) * 4 + 64 * 8 <= BYTES, "where a wave parks its sums");
+};
 
 template <int D, int MOD, int NB>
 __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(mx4_decode_waves(D, NB), mx4_decode_waves(D, NB)))) mx4_decode_kernel(const Mx4DecodeParams p) {
   constexpr int KS = D / 32;                       // steps of the first contraction
   constexpr int CH = D / 16;                       // channels of a lane in the second
-  __shared__ float park[4][CH * 4 * 64];
-  __shared__ float2 park_ml[4][64];
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = lane >> 4, m = lane & 15;
+  typedef Mx4Ring<D, NB> R;
+  extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
 
-  int split, bhk, hk, b;
-  p.by_split.split(blockIdx.x, bhk, split);
-  p.by_hkv.split(bhk, b, hk);
   const int group = (int)p.by_group.d, ncol = p.T * group;
+  const float c_scale = p.scale * kLog2e;
+  const int64_t codes_bytes = (int64_t)p.cache.page_size * (D / 2);
+  const int lane = threadIdx.x & 63, g = lane >> 4, m = lane & 15;
+  // workgroups go out to the eight XCDs in turn: an XCD takes neighbours, whose kv heads share the lines of memory in which one's part of a page ends and
+  // the next one's begins (64 sequences of 4k - 8k tokens, 32 / 8 heads, D = 128: 87.7 -> 86.5 us)
+  const int place = (gridDim.x & 7) == 0 ? (int)((blockIdx.x & 7) * (gridDim.x >> 3) + (blockIdx.x >> 3)) : (int)blockIdx.x;
+  int split, bhk, hk, b;
+  p.by_split.split(place, bhk, split);
+  p.by_hkv.split(bhk, b, hk);
   const int len = min(max(p.seq_lens[b], 0), p.max_len);
-  int row[NB], hq[NB], pos[NB];
-  bool live[NB];
+  const int t_lo = p.window >= 0 ? max(0, len - p.T - p.window) / 32 : 0, t_hi = (len + 31) / 32;
+  const int per_split = p.by_split.div(t_hi - t_lo + p.nsplit - 1);   // (a sequence without tiles: t_lo <= t_hi all the same)
+  const int t_begin = t_lo + split * per_split, t_end = min(t_hi, t_begin + per_split);
+  int row[NB], hq[NB], pos[NB];                    // (columns behind the last pair are copies of it)
 #pragma unroll
   for (int nb = 0; nb < NB; ++nb) {
-    const int c = 16 * nb + m;
-    live[nb] = c < ncol;
     int head;
-    p.by_group.split(live[nb] ? c : ncol - 1, row[nb], head);
+    p.by_group.split(min(16 * nb + m, ncol - 1), row[nb], head);
     hq[nb] = hk * group + head;
     pos[nb] = len - p.T + row[nb];
   }
-  const int first_key = p.window >= 0 ? max(0, len - p.T - p.window) : 0;
   const int first_full = p.window >= 0 ? max(0, len - 1 - p.window) : 0;
-  const int t_lo = first_key / 32, t_hi = (len + 31) / 32;
-  const int per_split = p.by_split.div(t_hi - t_lo + p.nsplit - 1);
-  const int t_begin = t_lo + split * per_split, t_end = min(t_hi, t_begin + per_split);
 
   bf16x8 qf[NB][KS];
   float slope2[NB], m_run[NB], l_run[NB];
@@ -116,54 +138,87 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(mx4_de
 #pragma unroll
     for (int c = 0; c < CH; ++c) oacc[nb][c] = (f32x4){0.f, 0.f, 0.f, 0.f};
   }
-  const float c_scale = p.scale * kLog2e;
-  const int64_t codes_bytes = (int64_t)p.cache.page_size * (D / 2);
 
-  // A lane's page of its eight keys of tile t in either contraction (an octet lies in one page; behind the sequence: its last one).  The entries of a
-  // tile are requested two tiles ahead of its products, its codes and scales one tile ahead.  The tile behind a wave's last is the last again: a load
-  // that is not there on one path would make the compiler wait for every load on the other.
-  const int t_last = t_begin + wave + max(0, t_end - 1 - t_begin - wave) / 4 * 4;
+  // The wave's tiles come through its ring in LDS, STAGES - 1 of them ahead of the one in use, by loads that need no registers.  In every one of them lane (g, m)
+  // fetches from octet m / 4 of the tile's keys (an octet lies in one page; behind the sequence: its last one), so that a tile is one table entry a lane:
+  //   keys     D = 128: the lane's own 16 bytes of keys m % 4 and 4 + m % 4; D = 64: the half g % 2 of key 4 (g / 2) + m % 4
+  //   values   rows of D / 2 bytes, the four octets' rows of one number next to each other: eight reads without bank conflicts
+  //   scales   a dword each
+  // The entries come the same way, for 16 tiles at a time.
+  unsigned char* const ring = lds + wave * R::BYTES;
+  const uint32_t ring_at = (uint32_t)(uintptr_t)(lds_void*)ring;
+  const int n_all = t_end - t_begin, n_each = (n_all + 3) / 4, t0 = t_begin + wave * n_each, n = min(n_each, n_all - wave * n_each);
   const int32_t* const table = p.block_table + (p.block_table != nullptr ? (int64_t)b * p.table_stride : 0);
-  const int in_page = p.block_table != nullptr ? (1 << p.page_shift) - 1 : -1;
-  struct Pages {
-    int k, v;
+  const int last_octet = (len - 1) & ~7, in_page = p.block_table != nullptr ? (1 << p.page_shift) - 1 : -1;
+  const int oct8 = (m >> 2) * 8;
+  const uint8_t *k_lane = p.cache.k + hk * p.cache.k_sh, *v_lane = p.cache.v + hk * p.cache.v_sh;
+  const bool v_scale = lane >= 32;
+  const uint8_t* const e_lane = (v_scale ? v_lane : k_lane) + codes_bytes +
+                                (int64_t)((lane >> 1 & 1) + (D == 128 ? (lane >> 4 & 1) * 2 : 0)) * p.cache.page_size + (lane & 1) * 4;
+  const uint32_t e_sp = (uint32_t)(v_scale ? p.cache.v_sp : p.cache.k_sp), k_sp = (uint32_t)p.cache.k_sp, v_sp = (uint32_t)p.cache.v_sp;
+  k_lane += D == 128 ? (m & 3) * 64 + g * 16 : (m & 3) * 32 + (g & 1) * 16 + (g >> 1) * 128;
+  v_lane += D == 128 ? g * 64 + (m & 3) * 16 : (2 * g + (m >> 1 & 1)) * 32 + (m & 1) * 16;
+  auto fetch_entries = [&](int w) __attribute__((always_inline)) {               // of tiles 16 w .. of this wave
+    const int j = min((t0 + 16 * w) * 32 + lane * 8, last_octet);
+    __builtin_amdgcn_global_load_lds((global_cvoid*)(table + (j >> p.page_shift)), (lds_void*)(ring + R::ENTRIES + (w & 1) * 256), 4, 0, 0);
   };
-  auto octet = [&](int t, int o) __attribute__((always_inline)) { return min(min(t, t_last) * 32 + 8 * o, (len - 1) & ~7); };
-  auto lookup = [&](int t) __attribute__((always_inline)) -> Pages {
-    if (p.block_table == nullptr) return {b, b};
-    return {table[octet(t, m >> 2) >> p.page_shift], table[octet(t, g) >> p.page_shift]};
+  auto fetch = [&](int i, int entry) __attribute__((always_inline)) {            // tile i of this wave
+    unsigned char* st = ring + i % R::STAGES * R::STAGE;
+    const uint32_t page = p.block_table != nullptr ? (uint32_t)min(max(entry, 0), p.num_pages - 1) : (uint32_t)b;
+    const uint32_t within = (uint32_t)(min((t0 + i) * 32 + oct8, last_octet) & in_page);
+    const uint8_t* kp = k_lane + (uint64_t)page * k_sp + (uint64_t)within * (D / 2);
+    const uint8_t* vp = v_lane + (uint64_t)page * v_sp + (uint64_t)within * (D / 2);
+    __builtin_amdgcn_global_load_lds((global_cvoid*)kp, (lds_void*)st, 16, 0, 0);
+    if (D == 128) __builtin_amdgcn_global_load_lds((global_cvoid*)kp, (lds_void*)(st + 1024 - 256), 16, 256, 0);   // (the offset counts on both sides)
+    __builtin_amdgcn_global_load_lds((global_cvoid*)vp, (lds_void*)(st + R::V), 16, 0, 0);
+    if (D == 128) __builtin_amdgcn_global_load_lds((global_cvoid*)vp, (lds_void*)(st + R::V + 1024 - 256), 16, 256, 0);
+    __builtin_amdgcn_global_load_lds((global_cvoid*)(e_lane + (uint64_t)page * e_sp + within), (lds_void*)(st + R::E), 4, 0, 0);
   };
   struct Tile {
-    uint32_t k[2][KS], v[8];
-    uint2 ke, ve;                                  // scales of eight keys of the lane's block
+    i32x4 k[2];                                    // D = 64: two dwords of each
+    uint32_t v[8];
+    i32x2 ke, ve;                                  // scales of eight keys of the lane's block
   };
-  const uint8_t* const k_lane = p.cache.k + hk * p.cache.k_sh + (m & 3) * (D / 2) + g * (D / 8);
-  const uint8_t* const v_lane = p.cache.v + hk * p.cache.v_sh + m * (CH / 2);
-  const uint8_t* const ke_lane = p.cache.k + hk * p.cache.k_sh + codes_bytes + (int64_t)(g * (D / 4) / 32) * p.cache.page_size;
-  const uint8_t* const ve_lane = p.cache.v + hk * p.cache.v_sh + codes_bytes + (int64_t)(m * CH / 32) * p.cache.page_size;
-  auto load = [&](int t, const Pages& pages, Tile& x) __attribute__((always_inline)) {
-    const int last = p.num_pages - 1;
-    const int64_t k_page = min(max(pages.k, 0), last) * p.cache.k_sp, v_page = min(max(pages.v, 0), last) * p.cache.v_sp;
-    const int k_in = octet(t, m >> 2) & in_page, v_in = octet(t, g) & in_page;
-    const uint8_t* kp = k_lane + k_page + (int64_t)k_in * (D / 2);
-    const uint8_t* vp = v_lane + v_page + (int64_t)v_in * (D / 2);
-#pragma unroll
-    for (int u = 0; u < 2; ++u) {
-      if constexpr (D == 128) {
-        const uint4 y = *(const uint4*)(kp + 4 * u * (D / 2));
-        x.k[u][0] = y.x; x.k[u][1] = y.y; x.k[u][2] = y.z; x.k[u][3] = y.w;
-      } else {
-        const uint2 y = *(const uint2*)(kp + 4 * u * (D / 2));
-        x.k[u][0] = y.x; x.k[u][1] = y.y;
-      }
+  // where in a stage this lane reads
+  const uint32_t at_k = D == 128 ? lane * 16 : (g >> 1) * 256 + m * 16 + (g & 1) * 8, at_v = R::V + (D == 128 ? lane * 4 : g * 64 + m * 2);
+  auto e_at = [&](int which, int block, int o) __attribute__((always_inline)) {
+    return (uint32_t)(R::E + 4 * (which * 32 + (block >> 1) * 16 + o * 4 + (block & 1) * 2));
+  };
+  const uint32_t at_ke = e_at(0, g * (D / 4) / 32, m >> 2), at_ve = e_at(1, m * CH / 32, g);
+  // Everything the products of tile i need, and the entry of tile i + STAGES: reads and their wait in one block, which the compiler takes to be
+  // done where it ends (it would make any other read of the ring wait for all loads into it).
+  auto take = [&](int i, Tile& x, int& entry) __attribute__((always_inline)) {
+    const uint32_t st = ring_at + i % R::STAGES * R::STAGE, a = st + at_k, c = st + at_v, d = st + at_ke, e = st + at_ve;
+    const uint32_t f = ring_at + R::ENTRIES + ((i + R::STAGES) & 31) * 16 + (m >> 2) * 4;
+    if constexpr (D == 128) {
+      asm volatile(
+          "ds_read_b128 %0, %13\n\tds_read_b128 %1, %13 offset:1024\n\tds_read_b64 %2, %15\n\tds_read_b64 %3, %16\n\t"
+          "ds_read_b32 %4, %14\n\tds_read_b32 %5, %14 offset:256\n\tds_read_b32 %6, %14 offset:512\n\tds_read_b32 %7, %14 offset:768\n\t"
+          "ds_read_b32 %8, %14 offset:1024\n\tds_read_b32 %9, %14 offset:1280\n\tds_read_b32 %10, %14 offset:1536\n\tds_read_b32 %11, %14 offset:1792\n\t"
+          "ds_read_b32 %12, %17\n\ts_waitcnt lgkmcnt(0)"
+          : "=&v"(x.k[0]), "=&v"(x.k[1]), "=&v"(x.ke), "=&v"(x.ve), "=&v"(x.v[0]), "=&v"(x.v[1]), "=&v"(x.v[2]), "=&v"(x.v[3]), "=&v"(x.v[4]),
+            "=&v"(x.v[5]), "=&v"(x.v[6]), "=&v"(x.v[7]), "=&v"(entry)
+          : "v"(a), "v"(c), "v"(d), "v"(e), "v"(f)
+          : "memory");
+    } else {
+      i32x2 k0, k1;
+      asm volatile(
+          "ds_read_b64 %0, %13\n\tds_read_b64 %1, %13 offset:512\n\tds_read_b64 %2, %15\n\tds_read_b64 %3, %16\n\t"
+          "ds_read_u16 %4, %14\n\tds_read_u16 %5, %14 offset:32\n\tds_read_u16 %6, %14 offset:256\n\tds_read_u16 %7, %14 offset:288\n\t"
+          "ds_read_u16 %8, %14 offset:512\n\tds_read_u16 %9, %14 offset:544\n\tds_read_u16 %10, %14 offset:768\n\tds_read_u16 %11, %14 offset:800\n\t"
+          "ds_read_b32 %12, %17\n\ts_waitcnt lgkmcnt(0)"
+          : "=&v"(k0), "=&v"(k1), "=&v"(x.ke), "=&v"(x.ve), "=&v"(x.v[0]), "=&v"(x.v[1]), "=&v"(x.v[2]), "=&v"(x.v[3]), "=&v"(x.v[4]),
+            "=&v"(x.v[5]), "=&v"(x.v[6]), "=&v"(x.v[7]), "=&v"(entry)
+          : "v"(a), "v"(c), "v"(d), "v"(e), "v"(f)
+          : "memory");
+      x.k[0] = (i32x4){k0[0], k0[1], 0, 0};
+      x.k[1] = (i32x4){k1[0], k1[1], 0, 0};
     }
-    x.ke = *(const uint2*)(ke_lane + k_page + k_in);
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      if constexpr (D == 128) x.v[i] = *(const uint32_t*)(vp + i * (D / 2));
-      else x.v[i] = *(const uint16_t*)(vp + i * (D / 2));
-    }
-    x.ve = *(const uint2*)(ve_lane + v_page + v_in);
+  };
+  auto entry_of = [&](int i) __attribute__((always_inline)) {
+    int x;
+    asm volatile("ds_read_b32 %0, %1\n\ts_waitcnt lgkmcnt(0)" : "=&v"(x) : "v"(ring_at + R::ENTRIES + (i & 31) * 16 + (m >> 2) * 4) : "memory");
+    return x;
   };
 
   auto compute = [&](int t, const Tile& tile) __attribute__((always_inline)) {
@@ -172,10 +227,10 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(mx4_de
     for (int u = 0; u < 2; ++u) {
 #pragma unroll
       for (int nb = 0; nb < NB; ++nb) s[nb][u] = (f32x4){0.f, 0.f, 0.f, 0.f};
-      const float scale = mx4_scale_value(((u ? tile.ke.y : tile.ke.x) >> (8 * (m & 3))) & 255);
+      const float scale = mx4_scale_value(((uint32_t)tile.ke[u] >> (8 * (m & 3))) & 255);
 #pragma unroll
       for (int f = 0; f < KS; ++f) {
-        const bf16x8 a = __builtin_bit_cast(bf16x8, mx4_bf16x8(tile.k[u][f], scale));
+        const bf16x8 a = __builtin_bit_cast(bf16x8, mx4_bf16x8((uint32_t)tile.k[u][f], scale));
 #pragma unroll
         for (int nb = 0; nb < NB; ++nb) s[nb][u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, qf[nb][f], s[nb][u], 0, 0, 0);
       }
@@ -234,7 +289,7 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(mx4_de
     }
     float vs[8];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) vs[i] = mx4_scale_value(((i < 4 ? tile.ve.x : tile.ve.y) >> (8 * (i & 3))) & 255);
+    for (int i = 0; i < 8; ++i) vs[i] = mx4_scale_value(((uint32_t)tile.ve[i >> 2] >> (8 * (i & 3))) & 255);
     if (t * 32 + 32 > len) {
       // what lies behind the sequence's end in its last page is any bytes: finite, for P is zero there
 #pragma unroll
@@ -266,71 +321,80 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(mx4_de
     }
   };
 
-  int t = t_begin + wave;
-  if (t < t_end) {
-    Tile even, odd;
-    Pages ahead = lookup(t);
-    load(t, ahead, even);
-    ahead = lookup(t + 4);
-    while (true) {
-      load(t + 4, ahead, odd);
-      ahead = lookup(t + 8);
-      compute(t, even);
-      if ((t += 4) >= t_end) break;
-      load(t + 4, ahead, even);
-      ahead = lookup(t + 8);
-      compute(t, odd);
-      if ((t += 4) >= t_end) break;
+  if (n > 0) {
+    int entry = 0;
+    if (p.block_table != nullptr) {
+      fetch_entries(0);
+      wait_vm<0>();
+    }
+#pragma unroll
+    for (int i = 0; i < R::STAGES - 1; ++i) {
+      entry = entry_of(i);                         // (without a table: not used)
+      if (i < n) fetch(i, entry);
+    }
+    entry = entry_of(R::STAGES - 1);
+    for (int i = 0; i < n; ++i) {
+      if ((i & 15) == 0 && i + 16 < n && p.block_table != nullptr) fetch_entries(i / 16 + 1);      // (first asked for 16 - STAGES steps later)
+      if (i + R::STAGES - 1 < n) {
+        fetch(i + R::STAGES - 1, entry);
+        wait_vm<(R::STAGES - 1) * R::LOADS>();     // all but the STAGES - 1 younger tiles has landed
+      } else {
+        wait_vm<0>();
+      }
+      Tile x;
+      take(i, x, entry);
+      compute(t0 + i, x);
     }
   }
 
   // ---- merge of the waves, a column block at a time; wave i then holds channels CH (4 g + i) .. + CH - 1 of column m
+  auto park = [&](int w) __attribute__((always_inline)) { return (float*)(lds + w * R::BYTES); };
+  auto park_ml = [&](int w) __attribute__((always_inline)) { return (float2*)(lds + w * R::BYTES + CH * 4 * 64 * 4); };
 #pragma unroll
   for (int nb = 0; nb < NB; ++nb) {
-    if (nb > 0) __syncthreads();
+    if (nb > 0) __syncthreads();                   // everyone has read what was parked before
 #pragma unroll
-    for (int c = 0; c < CH; ++c)
+    for (int k = 0; k < CH; ++k)
 #pragma unroll
-      for (int r = 0; r < 4; ++r) park[wave][(c * 4 + r) * 64 + lane] = oacc[nb][c][r];
-    park_ml[wave][lane] = make_float2(m_run[nb], quarter_sum(l_run[nb]));
+      for (int r = 0; r < 4; ++r) park(wave)[(k * 4 + r) * 64 + lane] = oacc[nb][k][r];
+    park_ml(wave)[lane] = make_float2(m_run[nb], quarter_sum(l_run[nb]));
     __syncthreads();
     float m_all = -INFINITY, l_all = 0.f, wgt[4];
 #pragma unroll
-    for (int u = 0; u < 4; ++u) m_all = fmaxf(m_all, park_ml[u][lane].x);
+    for (int u = 0; u < 4; ++u) m_all = fmaxf(m_all, park_ml(u)[lane].x);
     const float m_safe = m_all == -INFINITY ? 0.f : m_all;
 #pragma unroll
     for (int u = 0; u < 4; ++u) {
-      const float2 ml = park_ml[u][lane];
+      const float2 ml = park_ml(u)[lane];
       wgt[u] = fast_exp2(ml.x - m_safe);
       l_all = fmaf(ml.y, wgt[u], l_all);
     }
-    const bool result = p.nsplit == 1;
+    const bool result = p.nsplit == 1;             // the only split of its sequence: no partials and no merge kernel
     const float inv = result ? (l_all > 0.f ? 1.f / l_all : 0.f) : 1.f;
     float x[CH];
 #pragma unroll
-    for (int c = 0; c < CH; ++c) {
-      x[c] = 0.f;
+    for (int k = 0; k < CH; ++k) {
+      x[k] = 0.f;
 #pragma unroll
-      for (int u = 0; u < 4; ++u) x[c] = fmaf(park[u][(c * 4 + wave) * 64 + lane], wgt[u], x[c]);
-      x[c] *= inv;
+      for (int u = 0; u < 4; ++u) x[k] = fmaf(park(u)[(k * 4 + wave) * 64 + lane], wgt[u], x[k]);
+      x[k] *= inv;
     }
+    if (16 * nb + m >= ncol) continue;
     const int64_t slot = (((int64_t)b * p.T + row[nb]) * p.H + hq[nb]) * p.nsplit + split;
     const int ch = CH * (4 * g + wave);
-    if (live[nb]) {
-      if (!result || p.out_f32) {
-        float* to = result ? (float*)p.out + b * p.o_sb + hq[nb] * p.o_sh + row[nb] * p.o_st + ch : p.part_o + slot * D + ch;
+    if (!result || p.out_f32) {
+      float* to = result ? (float*)p.out + b * p.o_sb + hq[nb] * p.o_sh + row[nb] * p.o_st + ch : p.part_o + slot * D + ch;
 #pragma unroll
-        for (int c = 0; c < CH; c += 4) *(float4*)(to + c) = make_float4(x[c], x[c + 1], x[c + 2], x[c + 3]);
-      } else {
-        uint16_t* to = (uint16_t*)p.out + b * p.o_sb + hq[nb] * p.o_sh + row[nb] * p.o_st + ch;
+      for (int k = 0; k < CH; k += 4) *(float4*)(to + k) = make_float4(x[k], x[k + 1], x[k + 2], x[k + 3]);
+    } else {
+      uint16_t* to = (uint16_t*)p.out + b * p.o_sb + hq[nb] * p.o_sh + row[nb] * p.o_st + ch;
 #pragma unroll
-        for (int c = 0; c < CH; c += 4) *(uint2*)(to + c) = make_uint2(pack_bf16(x[c], x[c + 1]), pack_bf16(x[c + 2], x[c + 3]));
-      }
-      if (wave == 0 && g == 0) {
-        if (!result) *(float2*)(p.part_ml + slot * 2) = make_float2(m_all, l_all);
-        else if (p.lse != nullptr)
-          p.lse[b * p.lse_sb + hq[nb] * p.lse_sh + row[nb] * p.lse_st] = l_all > 0.f ? (m_all + __log2f(l_all)) * kLn2 : -INFINITY;
-      }
+      for (int k = 0; k < CH; k += 4) *(uint2*)(to + k) = make_uint2(pack_bf16(x[k], x[k + 1]), pack_bf16(x[k + 2], x[k + 3]));
+    }
+    if (wave == 0 && g == 0) {
+      if (!result) *(float2*)(p.part_ml + slot * 2) = make_float2(m_all, l_all);
+      else if (p.lse != nullptr)
+        p.lse[b * p.lse_sb + hq[nb] * p.lse_sh + row[nb] * p.lse_st] = l_all > 0.f ? (m_all + __log2f(l_all)) * kLn2 : -INFINITY;
     }
   }
 }
