@@ -48,29 +48,34 @@ __device__ __forceinline__ float mx4_cut(double x) {
   return __uint_as_float(u);
 }
 
-// Sixteen neighbouring channels, of which lane ^ 1 has the other half of the block: their codes, channel 0 lowest, and the scale byte.
-template <class F>
-__device__ __forceinline__ int mx4_pack16(F (&x)[16], uint32_t (&codes)[2]) {
+// NaN is held as zero (before the maximum, which passes over quiet ones only); the scale byte that these channels ask for by themselves: a block's is the
+// largest of its channels', since a scale grows with the magnitude.
+template <class F, int N>
+__device__ __forceinline__ int mx4_own_scale(F (&x)[N]) {
   F most = (F)0;
 #pragma unroll
-  for (int i = 0; i < 16; ++i) {
-    x[i] = x[i] != x[i] ? (F)0 : x[i];             // NaN is held as zero (here: the maximum passes over quiet ones only)
+  for (int i = 0; i < N; ++i) {
+    x[i] = x[i] != x[i] ? (F)0 : x[i];
     most = fmax(most, fabs(x[i]));
   }
-  most = fmax(most, __shfl_xor(most, 1));
-  const int e = mx4_scale(most);
+  return mx4_scale(most);
+}
+// the larger one of this lane's and lane ^ 1's (^ 2's)
+template <int CTRL>
+__device__ __forceinline__ int quad_max(int e) { return max(e, __builtin_amdgcn_update_dpp(0, e, CTRL, 0xF, 0xF, true)); }
+__device__ __forceinline__ int pair_max(int e) { return quad_max<0xB1>(e); }
+__device__ __forceinline__ int four_max(int e) { return quad_max<0x4E>(quad_max<0xB1>(e)); }
+
+// Eight neighbouring channels under the scale byte e, channel 0 lowest.
+template <class F>
+__device__ __forceinline__ uint32_t mx4_pack8(const F* y, int e) {
   const F unit = mx4_unit(e, (F)0);
-#pragma unroll
-  for (int w = 0; w < 2; ++w) {
-    const F* y = x + 8 * w;
-    uint32_t c = 0;
-    c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, mx4_cut(y[0] * unit), mx4_cut(y[1] * unit), 1.f, 0);
-    c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, mx4_cut(y[2] * unit), mx4_cut(y[3] * unit), 1.f, 1);
-    c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, mx4_cut(y[4] * unit), mx4_cut(y[5] * unit), 1.f, 2);
-    c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, mx4_cut(y[6] * unit), mx4_cut(y[7] * unit), 1.f, 3);
-    codes[w] = c;
-  }
-  return e;
+  uint32_t c = 0;
+  c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, mx4_cut(y[0] * unit), mx4_cut(y[1] * unit), 1.f, 0);
+  c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, mx4_cut(y[2] * unit), mx4_cut(y[3] * unit), 1.f, 1);
+  c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, mx4_cut(y[4] * unit), mx4_cut(y[5] * unit), 1.f, 2);
+  c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, mx4_cut(y[6] * unit), mx4_cut(y[7] * unit), 1.f, 3);
+  return c;
 }
 
 __device__ __forceinline__ float mx4_scale_value(int e) { return __uint_as_float((uint32_t)e << 23); }

@@ -35,14 +35,23 @@ RowShape shape_row(fl::NormParams* p, int dtype) {
   r.upl = r.wide ? (p->units <= 64 ? 1 : 4) : (p->units <= 128 ? 2 : 16);
   p->log_lanes = 0;
   while ((r.upl << p->log_lanes) < p->units) ++p->log_lanes;
-  p->tokens_per_block = 256 >> p->log_lanes;
+  p->by_pairs = fl::Divisor::of(p->pairs);
+  p->by_h = fl::Divisor::of(p->H);
+  p->by_hkv = fl::Divisor::of(p->Hkv);
   return r;
+}
+
+// Tokens of a workgroup: enough workgroups for the chip, then enough rows for long runs; their angles take LDS.
+constexpr int64_t kMostTokens = 16;
+int tokens_of(const fl::NormParams& p, int64_t workgroups) {
+  return (int)std::max<int64_t>(1, std::min<int64_t>({(int64_t)p.B * p.S / workgroups, kMostTokens, 16 * 1024 / p.pairs / 8}));
 }
 
 template <class T, int VEC, int UPL>
 hipError_t launch_forward(const fl::NormParams& p, bool il, dim3 grid, hipStream_t stream) {
-  if (il) hipLaunchKernelGGL((fl::norm_rotary_kernel<T, VEC, UPL, true>), grid, dim3(256), 0, stream, p);
-  else hipLaunchKernelGGL((fl::norm_rotary_kernel<T, VEC, UPL, false>), grid, dim3(256), 0, stream, p);
+  const size_t lds = fl::norm_lds_bytes(p.tokens_per_block, p.pairs, 4);
+  if (il) hipLaunchKernelGGL((fl::norm_rotary_kernel<T, VEC, UPL, true>), grid, dim3(256), lds, stream, p);
+  else hipLaunchKernelGGL((fl::norm_rotary_kernel<T, VEC, UPL, false>), grid, dim3(256), lds, stream, p);
   return hipGetLastError();
 }
 template <class T, int VEC, int UPL>
@@ -52,11 +61,13 @@ hipError_t launch_gradient(const fl::NormParams& p, bool il, dim3 grid, hipStrea
   else hipLaunchKernelGGL((fl::norm_rotary_bwd_kernel<T, VEC, UPL, false>), grid, dim3(256), lds, stream, p);
   return hipGetLastError();
 }
-template <int VEC, int UPL, bool MX4>
+template <int VEC, int UPL, bool MX4, bool ALIGNED = false>
 hipError_t launch_append(const fl::NormParams& p, bool il, dim3 grid, hipStream_t stream) {
-  const size_t lds = MX4 ? (size_t)p.tokens_per_block * p.D * sizeof(double) : 0;
-  if (il) hipLaunchKernelGGL((fl::norm_append_kernel<VEC, UPL, true, MX4>), grid, dim3(256), lds, stream, p);
-  else hipLaunchKernelGGL((fl::norm_append_kernel<VEC, UPL, false, MX4>), grid, dim3(256), lds, stream, p);
+  size_t lds = fl::norm_lds_bytes(p.tokens_per_block, p.pairs, 9);
+  if (MX4) lds += (size_t)p.tokens_per_block * p.pairs * 16;
+  if (MX4 && !ALIGNED) lds += (size_t)(256 >> p.log_lanes) * (p.D + 2) * sizeof(double);
+  if (il) hipLaunchKernelGGL((fl::norm_append_kernel<VEC, UPL, true, MX4, ALIGNED>), grid, dim3(256), lds, stream, p);
+  else hipLaunchKernelGGL((fl::norm_append_kernel<VEC, UPL, false, MX4, ALIGNED>), grid, dim3(256), lds, stream, p);
   return hipGetLastError();
 }
 
@@ -94,19 +105,14 @@ fl_status view_of(const fl_tensor* t, const char* name, const fl::NormParams& p,
   return st;
 }
 
-// Chunks of heads along y.
-void chunk_heads(fl::NormParams* p, int64_t blocks, bool append) {
-  p->heads_per_thread = rotary_heads(blocks, p->H + (append ? 2 : 1) * p->Hkv);
-  p->q_chunks = (p->H + p->heads_per_thread - 1) / p->heads_per_thread;
-  p->k_chunks = (p->Hkv + p->heads_per_thread - 1) / p->heads_per_thread;
-}
-
 // The gradient's launch: enough workgroups for the chip, few enough that their rows of partial sums are soon added up.
 constexpr int64_t kGradientBlocks = 2048;
 void share_gradient(fl::NormParams* p) {
-  const int64_t tokens = (int64_t)p->B * p->S;
-  p->groups = (int)((tokens + p->tokens_per_block - 1) / p->tokens_per_block);
-  chunk_heads(p, p->groups, false);
+  p->tokens_per_block = 256 >> p->log_lanes;
+  p->groups = (int)(((int64_t)p->B * p->S + p->tokens_per_block - 1) / p->tokens_per_block);
+  p->heads_per_thread = rotary_heads(p->groups, p->H + p->Hkv);
+  p->q_chunks = (p->H + p->heads_per_thread - 1) / p->heads_per_thread;
+  p->k_chunks = (p->Hkv + p->heads_per_thread - 1) / p->heads_per_thread;
   p->blocks = (int)std::max<int64_t>(1, std::min<int64_t>(p->groups, kGradientBlocks / std::max(1, p->q_chunks + p->k_chunks)));
 }
 
@@ -128,9 +134,8 @@ fl_status fl_norm_rotary(const fl_tensor* q, const fl_tensor* k, const fl_rotary
       (st = view_of(k, "k", p, true, dtype, &p.k)) != FL_OK || (st = view_of(k_out, "k_out", p, true, dtype, &p.k_out)) != FL_OK)
     return st;
   const RowShape r = shape_row(&p, dtype);
-  const int64_t blocks = ((int64_t)p.B * p.S + p.tokens_per_block - 1) / p.tokens_per_block;
-  chunk_heads(&p, blocks, false);
-  const dim3 grid((unsigned)blocks, (unsigned)(p.q_chunks + p.k_chunks));
+  p.tokens_per_block = tokens_of(p, 2048);
+  const dim3 grid((unsigned)(((int64_t)p.B * p.S + p.tokens_per_block - 1) / p.tokens_per_block));
   const bool il = rotary->interleaved != 0;
   hipStream_t s = (hipStream_t)stream;
   hipError_t e;
@@ -260,13 +265,18 @@ fl_status fl_norm_rotary_append(const fl_tensor* q, const fl_tensor* k, const fl
   p.seq_lens = kv->seq_lens;
   p.max_len = kv->max_seq_len;
   const RowShape r = shape_row(&p, FL_BF16);
-  const int64_t blocks = (B * T + p.tokens_per_block - 1) / p.tokens_per_block;
-  chunk_heads(&p, blocks, true);
-  const dim3 grid((unsigned)blocks, (unsigned)(p.q_chunks + 2 * p.k_chunks));
+  p.tokens_per_block = tokens_of(p, 256);
+  const int64_t blocks = (B * T + p.tokens_per_block - 1) / p.tokens_per_block, rows = p.tokens_per_block * (H + 2 * Hkv), at_once = 256 >> p.log_lanes;
+  // a column of workgroups shares its tokens' rows, down to one for each group of lanes, while that leaves a compute unit three workgroups at most (8 x 512 tokens,
+  // 32 / 8 heads, D = 128, into 4 bits, 16 tokens a column: 512 or 768 workgroups 24.4 us, 1024 27.1, 1536 27.3)
+  const int64_t parts = std::max<int64_t>(1, std::min<int64_t>((rows + at_once - 1) / at_once, (768 + blocks - 1) / blocks));
+  p.rows_per_part = (int)((rows + parts - 1) / parts);
+  const dim3 grid((unsigned)blocks, (unsigned)parts);
   const bool il = rotary->interleaved != 0;
   hipStream_t s = (hipStream_t)stream;
   hipError_t e;
-  if (mx4) e = r.wide ? launch_append<8, 1, true>(p, il, grid, s) : launch_append<1, 2, true>(p, il, grid, s);   // (D is 64 or 128)
+  if (mx4)                                         // (D is 64 or 128)
+    e = !r.wide ? launch_append<1, 2, true>(p, il, grid, s) : (p.pairs % 32 == 0 ? launch_append<8, 1, true, true>(p, il, grid, s) : launch_append<8, 1, true>(p, il, grid, s));
   else
     e = r.wide ? (r.upl == 1 ? launch_append<8, 1, false>(p, il, grid, s) : launch_append<8, 4, false>(p, il, grid, s))
                : (r.upl == 2 ? launch_append<1, 2, false>(p, il, grid, s) : launch_append<1, 16, false>(p, il, grid, s));

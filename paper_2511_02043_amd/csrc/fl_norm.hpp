@@ -4,9 +4,11 @@
 //     y = R(t) z,   z = w r x,   r = (mean_c x_c^2 + eps)^(-1/2),
 // with R the turn of channel pairs by the positions' angles (fl_rotary.hpp).  Its gradient, with dz = R(-t) dy and g = w dz:
 //     dx = r g - r^3 mean_c(x_c g_c) x,     dw = sum over tokens and heads of r x dz.
-// An element is read once (the gradient: x and dy) and written once, at some twenty operations: memory traffic, if the row's sum costs no second pass.  A
-// row therefore lies in the registers of a few lanes: lane `sub` of a group of `lanes` has the row's pairs sub VEC .. (two pieces of VEC channels, 16 bytes
-// each, at D = 128 eight lanes), the sum is three exchanges between neighbours, and the angles, formed once, serve several heads of the token.
+// An element is read once (the gradient: x and dy) and written once, at some twenty operations: memory traffic, if the row's sum costs no second pass and the
+// angles little.  A row therefore lies in the registers of a few lanes: lane `sub` of a group of them has the row's pairs sub VEC .. (two pieces of VEC channels,
+// 16 bytes each, at D = 128 eight lanes), and the sum is three exchanges between neighbours.  Forwards a workgroup has some tokens: it forms their angles
+// once, one (token, pair) a thread, keeps them in LDS, and goes through the rows in the order of memory, heads of a token first, so that its waves read and
+// write long runs (2 x 8192 tokens, 32 / 8 heads, D = 128, bf16: 70 us, 4.8 TB/s; lane groups that stay with a token and its angles, pieces of 256 bytes 12 KB apart, 81).
 #pragma once
 #include "fl_mx4.hpp"
 #include "fl_rotary.hpp"
@@ -18,13 +20,15 @@ struct NormParams : RotaryParams {
   float eps;
   int32_t norm;                    // 0: turns alone (appending only)
   int32_t log_lanes;               // lanes of a row: 2^log_lanes, times UPL at least the units
-  int32_t q_chunks, k_chunks;      // workgroups along y that take queries, keys (appending: then values), heads_per_thread heads each
+  Divisor by_pairs, by_h, by_hkv;
   // gradient
   View dy[2], dx[2];
+  int32_t q_chunks, k_chunks;      // workgroups along y that take queries, keys, heads_per_thread heads each
+  int32_t blocks, groups;          // workgroups along x; groups of tokens_per_block tokens that they share out
   float* part;                     // [q_chunks + k_chunks][blocks][D]: sums of dw; null: not wanted
-  float* dweight[2];               // [D] or null
-  int32_t blocks, groups;          // workgroups along x; token groups that they share out
+  float* dweight[2];               // [D], or null: not wanted
   // appending
+  int32_t rows_per_part;           // of the keys', queries' and values' rows of its tokens that a workgroup of a column takes
   Mx4Cache mx4;
   View k_held, v_held;             // what a cache in 4 bits holds for the new tokens; ptr null: not wanted
 };
@@ -48,11 +52,20 @@ __device__ __forceinline__ void group_sum(float (&x)[N], int lanes) {
       for (int i = 0; i < N; ++i) x[i] += __shfl_xor(x[i], o);
 }
 __device__ __forceinline__ double group_sum(double x, int lanes) {
-  for (int o = 1; o < lanes; o <<= 1) x += __shfl_xor(x, o);
+  auto dpp = [&](auto ctrl) __attribute__((always_inline)) {
+    const int lo = __builtin_amdgcn_update_dpp(0, __double2loint(x), decltype(ctrl)::value, 0xF, 0xF, true);
+    const int hi = __builtin_amdgcn_update_dpp(0, __double2hiint(x), decltype(ctrl)::value, 0xF, 0xF, true);
+    x += __hiloint2double(hi, lo);
+  };
+  if (lanes > 1) dpp(std::integral_constant<int, 0xB1>{});
+  if (lanes > 2) dpp(std::integral_constant<int, 0x4E>{});
+  if (lanes > 4) dpp(std::integral_constant<int, 0x141>{});
+  if (lanes > 8) dpp(std::integral_constant<int, 0x140>{});
+  for (int o = 16; o < lanes; o <<= 1) x += __shfl_xor(x, o);
   return x;
 }
 
-// What a lane has of every row of its token: UPL units of VEC pairs, or of VEC channels that stay (x1 unused then).
+// What a lane has of every row: UPL units of VEC pairs, or of VEC channels that stay (x1 unused then).
 template <class T, int VEC, int UPL, bool INTERLEAVED>
 struct NormLane {
   typedef RotaryPiece<T, VEC> Piece;
@@ -96,22 +109,6 @@ struct NormLane {
         w1[n][j] = w != nullptr ? w[at1[n] + j] : 1.f;
       }
   }
-  // in whole turns, reduced in 64 bits
-  __device__ __forceinline__ static double turn_of(const NormParams& p, const int32_t (&pos)[4], int pair) {
-    const int32_t at = pair < p.ends[0] ? pos[0] : (pair < p.ends[1] ? pos[1] : (pair < p.ends[2] ? pos[2] : pos[3]));
-    const double turn = (double)at * ((double)p.inv_freq[pair] * 0.15915494309189533577);
-    return turn - rint(turn);
-  }
-  __device__ __forceinline__ void angles(const NormParams& p, const int32_t (&pos)[4], int sub, float (&cs)[UPL][VEC], float (&sn)[UPL][VEC]) const {
-#pragma unroll
-    for (int n = 0; n < UPL; ++n)
-#pragma unroll
-      for (int j = 0; j < VEC; ++j) {
-        cs[n][j] = 1.f;
-        sn[n][j] = 0.f;
-        if (turns[n]) E::sincos_turns((float)turn_of(p, pos, (sub + n * lanes) * VEC + j), sn[n][j], cs[n][j]);
-      }
-  }
   // channels of pair j of a unit: (first piece, element) and (second piece, element)
   template <class P>
   __device__ __forceinline__ static auto& a_of(P& x0, P& x1, int j) { return INTERLEAVED ? (2 * j < VEC ? x0[(2 * j) % VEC] : x1[(2 * j) % VEC]) : x0[j]; }
@@ -128,27 +125,51 @@ __device__ __forceinline__ void wave_order() {
   __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
 }
 
-__device__ __forceinline__ void token_positions(const RotaryParams& p, int b, int s, int32_t (&pos)[4]) {
-#pragma unroll
-  for (int a = 0; a < 4; ++a) pos[a] = a < p.axes ? p.positions[b * p.pos_sb + s * p.pos_ss + a * p.pos_sa] : 0;
+// The angle of a token and channel pair in whole turns, reduced in 64 bits.
+__device__ __forceinline__ double turn_of(const NormParams& p, int token, int pair) {
+  int b, s;
+  p.by_s.split(token, b, s);
+  const int axis = pair < p.ends[0] ? 0 : (pair < p.ends[1] ? 1 : (pair < p.ends[2] ? 2 : 3));
+  const double turn = (double)p.positions[b * p.pos_sb + s * p.pos_ss + axis * p.pos_sa] * ((double)p.inv_freq[pair] * 0.15915494309189533577);
+  return turn - rint(turn);
 }
+// ... and sine and cosine of all pairs of n tokens from `token` on, [token][pair]
+template <class T>
+__device__ __forceinline__ void form_angles(const NormParams& p, int token, int n, float* cs, float* sn) {
+  for (int i = threadIdx.x; i < n * p.pairs; i += 256) {
+    int t, pair;
+    p.by_pairs.split(i, t, pair);
+    float c, x;
+    RotaryElem<T>::sincos_turns((float)turn_of(p, token + t, pair), x, c);
+    cs[i] = c;
+    sn[i] = x;
+  }
+}
+__device__ __forceinline__ int64_t row_at(const View& v, int b, int s) { return b * v.sb + s * v.ss; }
 
-// Heads [h, h_end) of one token: normalised, weighted and turned from `in` to `out` (null: computed for nobody).
-template <class T, int VEC, int UPL, bool INTERLEAVED>
-__device__ __forceinline__ void norm_rows(const NormParams& p, const NormLane<T, VEC, UPL, INTERLEAVED>& l, const T* in, int64_t in_sh, T* out, int64_t out_sh,
-                                          const float* weight, int h, int h_end, const float (&cs)[UPL][VEC], const float (&sn)[UPL][VEC]) {
+// Rows [row, row_end) of a workgroup's tokens, `heads` to a token: normalised, weighted and turned from `in` to `out`.  at_in(t), at_out(t): where token t's
+// rows begin (at_out < 0: nowhere).
+template <class T, int VEC, int UPL, bool INTERLEAVED, class In, class Out>
+__device__ __forceinline__ void norm_rows(const NormParams& p, const NormLane<T, VEC, UPL, INTERLEAVED>& l, int sub, const T* in, int64_t in_sh, In at_in, T* out,
+                                          int64_t out_sh, Out at_out, const float* weight, const Divisor& by_heads, int row, int row_end, const float* cs,
+                                          const float* sn) {
 #pragma clang fp contract(off)                     // one rounding order in training and in serving
   typedef NormLane<T, VEC, UPL, INTERLEAVED> L;
   typedef RotaryElem<T> E;
-  constexpr int HU = UPL * VEC <= 8 ? 4 : 1;       // heads whose loads are in flight together
+  constexpr int HU = UPL * VEC <= 8 ? 2 : 1;       // rows whose loads are in flight together
+  const int step = 256 >> p.log_lanes;
   float w0[UPL][VEC], w1[UPL][VEC];
   l.weights(weight, w0, w1);
   const float inv_d = 1.f / p.D;
-  for (int h0 = h; h0 < h_end; h0 += HU) {
+  for (int r0 = row + (threadIdx.x >> p.log_lanes); r0 < row_end; r0 += HU * step) {
     typename L::Piece x0[HU][UPL], x1[HU][UPL];
+    int t[HU], h[HU];
     float sum[HU] = {};
 #pragma unroll
-    for (int u = 0; u < HU; ++u) l.load(in + min(h0 + u, h_end - 1) * in_sh, x0[u], x1[u]);
+    for (int u = 0; u < HU; ++u) {
+      by_heads.split(min(r0 + u * step, row_end - 1), t[u], h[u]);
+      if (r0 + u * step < row_end) l.load(in + at_in(t[u]) + h[u] * in_sh, x0[u], x1[u]);
+    }
     if (p.norm) {
 #pragma unroll
       for (int u = 0; u < HU; ++u)
@@ -164,7 +185,7 @@ __device__ __forceinline__ void norm_rows(const NormParams& p, const NormLane<T,
     }
 #pragma unroll
     for (int u = 0; u < HU; ++u) {
-      if (h0 + u >= h_end) break;
+      if (r0 + u * step >= row_end) break;
       const float r = p.norm ? 1.f / sqrtf(fmaf(sum[u], inv_d, p.eps)) : 1.f;
 #pragma unroll
       for (int n = 0; n < UPL; ++n) {
@@ -175,12 +196,13 @@ __device__ __forceinline__ void norm_rows(const NormParams& p, const NormLane<T,
           z1[j] = E::load(x1[u][n].x[j]) * r * w1[n][j];
         }
         if (l.turns[n]) {
+          const int first = t[u] * p.pairs + (sub + n * l.lanes) * VEC;
 #pragma unroll
           for (int j = 0; j < VEC; ++j) {
             float &a = L::a_of(z0, z1, j), &c = L::b_of(z0, z1, j);
-            const float a_in = a, c_in = c;
-            a = fmaf(a_in, cs[n][j], -(c_in * sn[n][j]));
-            c = fmaf(c_in, cs[n][j], a_in * sn[n][j]);
+            const float a_in = a, c_in = c, co = cs[first + j], si = sn[first + j];
+            a = fmaf(a_in, co, -(c_in * si));
+            c = fmaf(c_in, co, a_in * si);
           }
         }
 #pragma unroll
@@ -189,33 +211,60 @@ __device__ __forceinline__ void norm_rows(const NormParams& p, const NormLane<T,
           x1[u][n].x[j] = E::store(z1[j]);
         }
       }
-      if (out != nullptr) l.store(out + (h0 + u) * out_sh, x0[u], x1[u]);
+      const int64_t to = at_out(t[u]);
+      if (to >= 0) l.store(out + to + h[u] * out_sh, x0[u], x1[u]);
     }
   }
 }
 
+// A workgroup's LDS: cosines and sines [tokens][pairs], then `places` numbers a token, where its rows begin, then what a kernel has beside.
+struct NormLds {
+  float *cs, *sn;
+  int64_t* at;
+  void* rest;
+};
+__device__ __forceinline__ NormLds norm_lds(const NormParams& p, void* base, int places) {
+  NormLds x;
+  x.cs = (float*)base;
+  x.sn = x.cs + p.tokens_per_block * p.pairs;
+  x.at = (int64_t*)(x.sn + p.tokens_per_block * p.pairs);
+  x.rest = x.at + places * p.tokens_per_block;
+  return x;
+}
+constexpr size_t norm_lds_bytes(int tokens, int pairs, int places) { return (size_t)tokens * (pairs * 8 + places * 8); }
+
 template <class T, int VEC, int UPL, bool INTERLEAVED>
 __global__ void __launch_bounds__(256) norm_rotary_kernel(const NormParams p) {
-  const int sub = threadIdx.x & ((1 << p.log_lanes) - 1), local = threadIdx.x >> p.log_lanes;
-  const int64_t token = (int64_t)blockIdx.x * p.tokens_per_block + local;
-  if (token >= (int64_t)p.B * p.S) return;         // (whole groups of lanes)
-  int b, s;
-  p.by_s.split((int)token, b, s);
-  int32_t pos[4];
-  token_positions(p, b, s, pos);
+  extern __shared__ int64_t norm_shared[];
+  const NormLds x = norm_lds(p, norm_shared, 4);
+  const int sub = threadIdx.x & ((1 << p.log_lanes) - 1);
+  const int token = blockIdx.x * p.tokens_per_block, n = min(p.tokens_per_block, p.B * p.S - token);
+  if ((int)threadIdx.x < n) {
+    int b, s;
+    p.by_s.split(token + threadIdx.x, b, s);
+    int64_t* at = x.at + 4 * threadIdx.x;
+    at[0] = row_at(p.q, b, s);
+    at[1] = row_at(p.q_out, b, s);
+    at[2] = row_at(p.k, b, s);
+    at[3] = row_at(p.k_out, b, s);
+  }
+  form_angles<T>(p, token, n, x.cs, x.sn);
+  __syncthreads();
   NormLane<T, VEC, UPL, INTERLEAVED> l;
   l.init(p, sub);
-  float cs[UPL][VEC], sn[UPL][VEC];
-  l.angles(p, pos, sub, cs, sn);
-  const bool keys = (int)blockIdx.y >= p.q_chunks;
-  const int heads = keys ? p.Hkv : p.H, h = (blockIdx.y - (keys ? p.q_chunks : 0)) * p.heads_per_thread;
-  const View &in = keys ? p.k : p.q, &out = keys ? p.k_out : p.q_out;
-  norm_rows<T, VEC, UPL, INTERLEAVED>(p, l, (const T*)in.ptr + b * in.sb + s * in.ss, in.sh, (T*)out.ptr + b * out.sb + s * out.ss, out.sh, p.weight[keys],
-                                      h, min(h + p.heads_per_thread, heads), cs, sn);
+  auto rows = [&](const View& in, const View& out, int place, int heads, const Divisor& by, const float* weight) __attribute__((always_inline)) {
+    norm_rows<T, VEC, UPL, INTERLEAVED>(p, l, sub, (const T*)in.ptr, in.sh, [&](int t) { return x.at[4 * t + place]; }, (T*)out.ptr, out.sh,
+                                        [&](int t) { return x.at[4 * t + place + 1]; }, weight, by, 0, n * heads, x.cs, x.sn);
+  };
+  rows(p.q, p.q_out, 0, p.H, p.by_h, p.weight[0]);
+  rows(p.k, p.k_out, 2, p.Hkv, p.by_hkv, p.weight[1]);
 }
 
-// The gradient.  A workgroup goes through groups of 256 / lanes tokens, one workgroup a chunk of heads; dw gathers in registers, then over the workgroup's tokens in
-// LDS, and leaves as a row of partial sums for norm_weights_kernel: no atomics, so that the result does not depend on who comes first.
+// The gradient.  Its rows' angles stay in registers: a group of lanes keeps to a token and goes through the chunk of heads that the workgroup has of it, the next
+// head's rows on their way while one is worked on.  (us with the rows shared out as in the forward pass / so: 2 x 8192 tokens, 32 / 8 heads, D = 128 121 / 118,
+// D = 64 71 / 63, 512 tokens 18 / 15; here the exchange with LDS and the places of a row cost more than the runs give.)
+// dw gathers in registers, then over the workgroup in LDS, and leaves as a row of partial sums for norm_weights_kernel: no atomics, so that the result does
+// not depend on who comes first.
 template <class T, int VEC, int UPL, bool INTERLEAVED>
 __global__ void __launch_bounds__(256) norm_rotary_bwd_kernel(const NormParams p) {
   typedef NormLane<T, VEC, UPL, INTERLEAVED> L;
@@ -236,66 +285,68 @@ __global__ void __launch_bounds__(256) norm_rotary_bwd_kernel(const NormParams p
     if (token >= (int64_t)p.B * p.S) continue;     // (whole groups of lanes)
     int b, s;
     p.by_s.split((int)token, b, s);
-    int32_t pos[4];
-    token_positions(p, b, s, pos);
     float cs[UPL][VEC], sn[UPL][VEC];
-    l.angles(p, pos, sub, cs, sn);
-    const T* x_in = (const T*)xv.ptr + b * xv.sb + s * xv.ss;
-    const T* y_in = (const T*)yv.ptr + b * yv.sb + s * yv.ss;
-    T* out = (T*)ov.ptr + b * ov.sb + s * ov.ss;
-    constexpr int HU = UPL * VEC <= 8 ? 2 : 1;
-    for (int h0 = h_begin; h0 < h_end; h0 += HU) {
-      typename L::Piece x0[HU][UPL], x1[HU][UPL], y0[HU][UPL], y1[HU][UPL];
 #pragma unroll
-      for (int u = 0; u < HU; ++u) {
-        const int h = min(h0 + u, h_end - 1);
-        l.load(x_in + h * xv.sh, x0[u], x1[u]);
-        l.load(y_in + h * yv.sh, y0[u], y1[u]);
+    for (int n = 0; n < UPL; ++n)
+#pragma unroll
+      for (int j = 0; j < VEC; ++j) {
+        cs[n][j] = 1.f;
+        sn[n][j] = 0.f;
+        if (l.turns[n]) E::sincos_turns((float)turn_of(p, (int)token, (sub + n * l.lanes) * VEC + j), sn[n][j], cs[n][j]);
       }
-      float sum[2 * HU] = {};                      // of x^2 and of x g
-      float z0[HU][UPL][VEC], z1[HU][UPL][VEC];    // dz
+    const T* x_in = (const T*)xv.ptr + row_at(xv, b, s);
+    const T* y_in = (const T*)yv.ptr + row_at(yv, b, s);
+    T* out = (T*)ov.ptr + row_at(ov, b, s);
+    typename L::Piece x0[UPL], x1[UPL], y0[UPL], y1[UPL];
+    l.load(x_in + h_begin * xv.sh, x0, x1);
+    l.load(y_in + h_begin * yv.sh, y0, y1);
+    for (int h = h_begin; h < h_end; ++h) {
+      float sum[2] = {};                           // of x^2 and of x g
+      float z0[UPL][VEC], z1[UPL][VEC], a0[UPL][VEC], a1[UPL][VEC];                  // dz, x
 #pragma unroll
-      for (int u = 0; u < HU; ++u)
+      for (int n = 0; n < UPL; ++n) {
 #pragma unroll
-        for (int n = 0; n < UPL; ++n) {
+        for (int j = 0; j < VEC; ++j) {
+          a0[n][j] = l.has[n] ? E::load(x0[n].x[j]) : 0.f;
+          a1[n][j] = l.turns[n] ? E::load(x1[n].x[j]) : 0.f;
+          z0[n][j] = l.has[n] ? E::load(y0[n].x[j]) : 0.f;
+          z1[n][j] = l.turns[n] ? E::load(y1[n].x[j]) : 0.f;
+        }
+      }
+      const int next = min(h + 1, h_end - 1);
+      l.load(x_in + next * xv.sh, x0, x1);
+      l.load(y_in + next * yv.sh, y0, y1);
+#pragma unroll
+      for (int n = 0; n < UPL; ++n) {
+        if (l.turns[n]) {
 #pragma unroll
           for (int j = 0; j < VEC; ++j) {
-            z0[u][n][j] = l.has[n] ? E::load(y0[u][n].x[j]) : 0.f;
-            z1[u][n][j] = l.turns[n] ? E::load(y1[u][n].x[j]) : 0.f;
-          }
-          if (l.turns[n]) {
-#pragma unroll
-            for (int j = 0; j < VEC; ++j) {
-              float &a = L::a_of(z0[u][n], z1[u][n], j), &c = L::b_of(z0[u][n], z1[u][n], j);
-              const float a_in = a, c_in = c;
-              a = a_in * cs[n][j] + c_in * sn[n][j];
-              c = c_in * cs[n][j] - a_in * sn[n][j];
-            }
-          }
-#pragma unroll
-          for (int j = 0; j < VEC; ++j) {
-            const float a = l.has[n] ? E::load(x0[u][n].x[j]) : 0.f, c = l.turns[n] ? E::load(x1[u][n].x[j]) : 0.f;
-            sum[2 * u] = fmaf(a, a, fmaf(c, c, sum[2 * u]));
-            sum[2 * u + 1] = fmaf(a * w0[n][j], z0[u][n][j], fmaf(c * w1[n][j], z1[u][n][j], sum[2 * u + 1]));
+            float &a = L::a_of(z0[n], z1[n], j), &c = L::b_of(z0[n], z1[n], j);
+            const float a_in = a, c_in = c;
+            a = a_in * cs[n][j] + c_in * sn[n][j];
+            c = c_in * cs[n][j] - a_in * sn[n][j];
           }
         }
-      group_sum(sum, l.lanes);
 #pragma unroll
-      for (int u = 0; u < HU; ++u) {
-        if (h0 + u >= h_end) break;
-        const float r = 1.f / sqrtf(fmaf(sum[2 * u], inv_d, p.eps)), back = r * r * r * (sum[2 * u + 1] * inv_d);
-#pragma unroll
-        for (int n = 0; n < UPL; ++n)
-#pragma unroll
-          for (int j = 0; j < VEC; ++j) {
-            const float a = E::load(x0[u][n].x[j]), c = E::load(x1[u][n].x[j]);
-            d0[n][j] = fmaf(a * r, z0[u][n][j], d0[n][j]);
-            d1[n][j] = fmaf(c * r, z1[u][n][j], d1[n][j]);
-            x0[u][n].x[j] = E::store(fmaf(r * w0[n][j], z0[u][n][j], -a * back));
-            x1[u][n].x[j] = E::store(fmaf(r * w1[n][j], z1[u][n][j], -c * back));
-          }
-        if (ov.ptr != nullptr) l.store(out + (h0 + u) * ov.sh, x0[u], x1[u]);
+        for (int j = 0; j < VEC; ++j) {
+          sum[0] = fmaf(a0[n][j], a0[n][j], fmaf(a1[n][j], a1[n][j], sum[0]));
+          sum[1] = fmaf(a0[n][j] * w0[n][j], z0[n][j], fmaf(a1[n][j] * w1[n][j], z1[n][j], sum[1]));
+        }
       }
+      group_sum(sum, l.lanes);
+      const float r = 1.f / sqrtf(fmaf(sum[0], inv_d, p.eps)), back = r * r * r * (sum[1] * inv_d);
+      typename L::Piece o0[UPL], o1[UPL];
+#pragma unroll
+      for (int n = 0; n < UPL; ++n)
+#pragma unroll
+        for (int j = 0; j < VEC; ++j) {
+          const float a = a0[n][j], c = a1[n][j];
+          d0[n][j] = fmaf(a * r, z0[n][j], d0[n][j]);
+          d1[n][j] = fmaf(c * r, z1[n][j], d1[n][j]);
+          o0[n].x[j] = E::store(fmaf(r * w0[n][j], z0[n][j], -a * back));
+          o1[n].x[j] = E::store(fmaf(r * w1[n][j], z1[n][j], -c * back));
+        }
+      if (ov.ptr != nullptr) l.store(out + h * ov.sh, o0, o1);
     }
   }
 
@@ -344,158 +395,207 @@ __global__ void __launch_bounds__(1024) norm_weights_kernel(const NormParams p) 
   if (threadIdx.x < 16 && c < p.D) p.dweight[which][c] = lds[threadIdx.x];
 }
 
-// New tokens in serving: queries out, keys and values into the pages of a bf16 cache or of one in 4 bits (MX4).  Chunks of heads along y: keys first,
-// whose way is the longest, then queries, then values.  A key that is held in 4 bits is computed in 64: its codes are those of the formula's
-// result, and do not depend on the kernel that wrote them.
-template <int VEC, int UPL, bool INTERLEAVED, bool MX4>
+// New tokens in serving: queries out, keys and values into the pages of a bf16 cache or of one in 4 bits (MX4).  A workgroup has some tokens, and of their
+// keys', queries' and values' rows, in this order, a part.  A key that is held in 4 bits is computed in 64: its codes are those of the formula's
+// result, and do not depend on the kernel that wrote them.  ALIGNED: a lane's pieces and its neighbours' make whole blocks of 32 channels (VEC = 8,
+// pairs a multiple of 32), so that a key goes from registers to the page; else it is put together in LDS.
+template <int VEC, int UPL, bool INTERLEAVED, bool MX4, bool ALIGNED>
 __global__ void __launch_bounds__(256) norm_append_kernel(const NormParams p) {
   typedef uint16_t T;
   typedef NormLane<T, VEC, UPL, INTERLEAVED> L;
   typedef RotaryElem<T> E;
-  extern __shared__ double key_lds[];              // MX4: a row of D for each group of lanes
-  const int sub = threadIdx.x & ((1 << p.log_lanes) - 1), local = threadIdx.x >> p.log_lanes;
-  const int64_t token = (int64_t)blockIdx.x * p.tokens_per_block + local;
-  const bool real = token < (int64_t)p.B * p.S;
-  int b = 0, s = 0;
-  if (real) p.by_s.split((int)token, b, s);
-  const int y = blockIdx.y;
-  const bool keys = y < p.k_chunks, queries = !keys && y < p.k_chunks + p.q_chunks;
-  const int h = (keys ? y : (queries ? y - p.k_chunks : y - p.k_chunks - p.q_chunks)) * p.heads_per_thread;
-  const int h_end = min(h + p.heads_per_thread, queries ? p.H : p.Hkv);
+  static_assert(!ALIGNED || (MX4 && VEC == 8 && UPL == 1), "pieces of eight channels");
+  extern __shared__ int64_t norm_shared[];
+  constexpr int PLACES = 9;                        // q, q_out, k, v, the pages of k and v (< 0: none), the tokens' numbers there, k_held and v_held
+  const NormLds x = norm_lds(p, norm_shared, PLACES);
+  double* const cs64 = (double*)x.rest;            // MX4: [tokens][pairs] again
+  double* const sn64 = cs64 + p.tokens_per_block * p.pairs;
+  const int sub = threadIdx.x & ((1 << p.log_lanes) - 1), step = 256 >> p.log_lanes;
+  const int token = blockIdx.x * p.tokens_per_block, n = min(p.tokens_per_block, p.B * p.S - token);
+  // this workgroup's keys [lo, hi), queries and values
+  const int part = blockIdx.y * p.rows_per_part, part_end = part + p.rows_per_part, n_k = n * p.Hkv, n_q = n * p.H;
+  auto cut = [&](int first, int rows, int& lo, int& hi) __attribute__((always_inline)) {
+    lo = min(max(part - first, 0), rows);
+    hi = min(max(part_end - first, 0), rows);
+  };
+  int k_lo, k_hi, q_lo, q_hi, v_lo, v_hi;
+  cut(0, n_k, k_lo, k_hi);
+  cut(n_k, n_q, q_lo, q_hi);
+  cut(n_k + n_q, n_k, v_lo, v_hi);
+
+  if ((int)threadIdx.x < n) {
+    int b, s;
+    p.by_s.split(token + threadIdx.x, b, s);
+    int64_t* at = x.at + PLACES * threadIdx.x;
+    at[0] = row_at(p.q, b, s);
+    at[1] = row_at(p.q_out, b, s);
+    at[2] = row_at(p.k, b, s);
+    at[3] = row_at(p.v, b, s);
+    at[7] = row_at(p.k_held, b, s);
+    at[8] = row_at(p.v_held, b, s);
+    // the token's slot (from the true length: cut to the bound it would be an older token's)
+    int64_t page = -1, within = 0;
+    if (k_lo < k_hi || v_lo < v_hi) {
+      const int slot = max(p.seq_lens[b], 0) - p.S + s;
+      if (slot >= 0 && slot < p.max_len) {
+        page = b, within = slot;
+        if (p.block_table != nullptr) {
+          page = p.block_table[(int64_t)b * p.table_stride + (slot >> p.page_shift)];
+          within = slot & ((1 << p.page_shift) - 1);
+        }
+        if (page >= p.num_pages) page = -1;
+      }
+    }
+    at[4] = page < 0 ? -1 : (MX4 ? page * p.mx4.k_sp : page * p.kc_sp + within * p.kc_st);
+    at[5] = page < 0 ? -1 : (MX4 ? page * p.mx4.v_sp : page * p.vc_sp + within * p.vc_st);
+    at[6] = within;
+  }
+  if (q_lo < q_hi || (!MX4 && k_lo < k_hi)) form_angles<T>(p, token, n, x.cs, x.sn);
+  if (MX4 && k_lo < k_hi) {
+    for (int i = threadIdx.x; i < n * p.pairs; i += 256) {
+      int t, pair;
+      p.by_pairs.split(i, t, pair);
+      double c, y;
+      sincospi(2. * turn_of(p, token + t, pair), &y, &c);
+      cs64[i] = c;
+      sn64[i] = y;
+    }
+  }
+  __syncthreads();
   L l;
   l.init(p, sub);
+  auto place = [&](int i) __attribute__((always_inline)) { return [=](int t) { return x.at[PLACES * t + i]; }; };
 
-  if (queries) {
-    if (!real) return;
-    int32_t pos[4];
-    token_positions(p, b, s, pos);
-    float cs[UPL][VEC], sn[UPL][VEC];
-    l.angles(p, pos, sub, cs, sn);
-    norm_rows<T, VEC, UPL, INTERLEAVED>(p, l, (const T*)p.q.ptr + b * p.q.sb + s * p.q.ss, p.q.sh, (T*)p.q_out.ptr + b * p.q_out.sb + s * p.q_out.ss, p.q_out.sh,
-                                        p.weight[0], h, h_end, cs, sn);
-    return;
-  }
-
-  // this token's slot (from the true length: cut to the bound it would be an older token's)
-  int64_t page = -1, within = 0;
-  if (real) {
-    const int slot = max(p.seq_lens[b], 0) - p.S + s;
-    if (slot >= 0 && slot < p.max_len) {
-      page = b, within = slot;
-      if (p.block_table != nullptr) {
-        page = p.block_table[(int64_t)b * p.table_stride + (slot >> p.page_shift)];
-        within = slot & ((1 << p.page_shift) - 1);
-      }
-      if (page >= p.num_pages) page = -1;
+  // Eight channels of a row of token t from channel `at` on under the block's scale byte e: to the page (base: of the head) and to the caller
+  const int D = p.D;
+  auto put = [&](uint32_t codes, int e, int at, int t, uint8_t* base, int which, const View& held, int head) __attribute__((always_inline)) {
+    const int64_t page = x.at[PLACES * t + 4 + which], within = x.at[PLACES * t + 6];
+    if (page >= 0) {
+      base += page;
+      *(uint32_t*)(base + within * (D / 2) + at / 2) = codes;
+      if ((at & 31) == 0) base[(int64_t)p.mx4.page_size * (D / 2) + (int64_t)(at >> 5) * p.mx4.page_size + within] = (uint8_t)e;
     }
-  }
+    if (held.ptr != nullptr) *(uint4*)((T*)held.ptr + x.at[PLACES * t + 7 + which] + head * held.sh + at) = mx4_bf16x8(codes, mx4_scale_value(e));
+  };
+  // sixteen channels, 16 sub .. (lanes from D / 16 on have none), lane ^ 1 has the other half of the block
+  auto put16 = [&](auto& y, int t, uint8_t* base, int which, const View& held, int head) __attribute__((always_inline)) {
+    const int e = pair_max(mx4_own_scale(y));
+    if (16 * sub >= D) return;
+    put(mx4_pack8(y, e), e, 16 * sub, t, base, which, held, head);
+    put(mx4_pack8(y + 8, e), e, 16 * sub + 8, t, base, which, held, head);
+  };
 
   if constexpr (!MX4) {
-    if (page < 0) return;
-    if (keys) {
-      int32_t pos[4];
-      token_positions(p, b, s, pos);
-      float cs[UPL][VEC], sn[UPL][VEC];
-      l.angles(p, pos, sub, cs, sn);
-      norm_rows<T, VEC, UPL, INTERLEAVED>(p, l, (const T*)p.k.ptr + b * p.k.sb + s * p.k.ss, p.k.sh, p.k_cache + page * p.kc_sp + within * p.kc_st, p.kc_sh,
-                                          p.weight[1], h, h_end, cs, sn);
-    } else {
-      const T* in = (const T*)p.v.ptr + b * p.v.sb + s * p.v.ss;
-      T* out = p.v_cache + page * p.vc_sp + within * p.vc_st;
-      for (int h0 = h; h0 < h_end; ++h0) {
-        typename L::Piece x0[UPL], x1[UPL];
-        l.load(in + h0 * p.v.sh, x0, x1);
-        l.store(out + h0 * p.vc_sh, x0, x1);
-      }
-    }
-  } else {
-    const int D = p.D;
-    // sixteen channels of a row, 16 sub .., to the cache and to the caller (lanes from D / 16 on have none)
-    auto put = [&](int head, auto& x, uint8_t* base, const View& held) __attribute__((always_inline)) {
-      uint32_t codes[2];
-      const int e = mx4_pack16(x, codes);
-      if (!real || 16 * sub >= D) return;
-      if (page >= 0) {
-        *(uint2*)(base + within * (D / 2) + 8 * sub) = make_uint2(codes[0], codes[1]);
-        if ((sub & 1) == 0) base[(int64_t)p.mx4.page_size * (D / 2) + (int64_t)(sub >> 1) * p.mx4.page_size + within] = (uint8_t)e;
-      }
-      if (held.ptr != nullptr) {
-        uint4* to = (uint4*)((T*)held.ptr + b * held.sb + head * held.sh + s * held.ss + 16 * sub);
-        to[0] = mx4_bf16x8(codes[0], mx4_scale_value(e));
-        to[1] = mx4_bf16x8(codes[1], mx4_scale_value(e));
-      }
-    };
-    if (!keys) {
-      const T* in = (const T*)p.v.ptr + b * p.v.sb + s * p.v.ss + (16 * sub < D ? 16 * sub : 0);
-      for (int h0 = h; h0 < h_end; ++h0) {
-        const RotaryPiece<T, 8> v0 = *(const RotaryPiece<T, 8>*)(in + h0 * p.v.sh), v1 = *(const RotaryPiece<T, 8>*)(in + h0 * p.v.sh + 8);
-        float x[16];
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          x[j] = E::load(v0.x[j]);
-          x[8 + j] = E::load(v1.x[j]);
-        }
-        put(h0, x, p.mx4.v + page * p.mx4.v_sp + h0 * p.mx4.v_sh, p.v_held);
-      }
-      return;
-    }
-    int32_t pos[4];
-    token_positions(p, b, s, pos);                 // (lanes behind the last token: the first one's)
-    double cs[UPL][VEC], sn[UPL][VEC];
-#pragma unroll
-    for (int n = 0; n < UPL; ++n)
-#pragma unroll
-      for (int j = 0; j < VEC; ++j) {
-        cs[n][j] = 1.;
-        sn[n][j] = 0.;
-        if (l.turns[n]) sincospi(2. * L::turn_of(p, pos, (sub + n * l.lanes) * VEC + j), &sn[n][j], &cs[n][j]);
-      }
+    norm_rows<T, VEC, UPL, INTERLEAVED>(p, l, sub, (const T*)p.k.ptr, p.k.sh, place(2), p.k_cache, p.kc_sh, place(4), p.weight[1], p.by_hkv, k_lo, k_hi, x.cs, x.sn);
+  } else if (k_lo < k_hi) {
     float w0[UPL][VEC], w1[UPL][VEC];
     l.weights(p.weight[1], w0, w1);
-    const T* in = (const T*)p.k.ptr + b * p.k.sb + s * p.k.ss;
-    double* const mine = key_lds + local * D;
-    for (int h0 = h; h0 < h_end; ++h0) {
-      typename L::Piece x0[UPL], x1[UPL];
-      l.load(in + h0 * p.k.sh, x0, x1);
-      double sum = 0.;
+    double* const mine = sn64 + p.tokens_per_block * p.pairs + (threadIdx.x >> p.log_lanes) * (D + 2);     // not ALIGNED: a row of this group of lanes
+    typename L::Piece x0[UPL], x1[UPL];
+    int t, h;
+    auto load = [&](int r) __attribute__((always_inline)) {
+      p.by_hkv.split(min(r, k_hi - 1), t, h);      // (groups behind the last row: that one again, for the exchanges between lanes; not stored)
+      l.load((const T*)p.k.ptr + x.at[PLACES * t + 2] + h * p.k.sh, x0, x1);
+    };
+    load(k_lo + (threadIdx.x >> p.log_lanes));
+    for (int r0 = k_lo; r0 < k_hi; r0 += step) {
+      const int r = r0 + (threadIdx.x >> p.log_lanes), t_now = t, h_now = h;
+      const bool real = r < k_hi;
+      double z0[UPL][VEC], z1[UPL][VEC], sum = 0.;
 #pragma unroll
       for (int n = 0; n < UPL; ++n)
 #pragma unroll
         for (int j = 0; j < VEC; ++j) {
-          const double a = l.has[n] ? (double)E::load(x0[n].x[j]) : 0., c = l.turns[n] ? (double)E::load(x1[n].x[j]) : 0.;
-          sum = fma(a, a, fma(c, c, sum));
+          z0[n][j] = l.has[n] ? (double)E::load(x0[n].x[j]) : 0.;
+          z1[n][j] = l.turns[n] ? (double)E::load(x1[n].x[j]) : 0.;
+          sum = fma(z0[n][j], z0[n][j], fma(z1[n][j], z1[n][j], sum));
         }
-      const double r = p.norm ? 1. / sqrt(group_sum(sum, l.lanes) / D + (double)p.eps) : 1.;
-      // (a row stays with its lanes, which lie in one wave: LDS keeps a wave's order)
-      wave_order();
+      if (r0 + step < k_hi) load(r + step);
+      const double rn = p.norm ? 1. / sqrt(group_sum(sum, l.lanes) / D + (double)p.eps) : 1.;
 #pragma unroll
       for (int n = 0; n < UPL; ++n) {
-        double z0[VEC], z1[VEC];
 #pragma unroll
         for (int j = 0; j < VEC; ++j) {
-          z0[j] = E::load(x0[n].x[j]) * r * w0[n][j];
-          z1[j] = E::load(x1[n].x[j]) * r * w1[n][j];
+          z0[n][j] *= rn * w0[n][j];
+          z1[n][j] *= rn * w1[n][j];
         }
         if (l.turns[n]) {
+          const int first = t_now * p.pairs + (sub + n * l.lanes) * VEC;
 #pragma unroll
           for (int j = 0; j < VEC; ++j) {
-            double &a = L::a_of(z0, z1, j), &c = L::b_of(z0, z1, j);
-            const double a_in = a, c_in = c;
-            a = a_in * cs[n][j] - c_in * sn[n][j];
-            c = c_in * cs[n][j] + a_in * sn[n][j];
+            double &a = L::a_of(z0[n], z1[n], j), &c = L::b_of(z0[n], z1[n], j);
+            const double a_in = a, c_in = c, co = cs64[first + j], si = sn64[first + j];
+            a = a_in * co - c_in * si;
+            c = c_in * co + a_in * si;
           }
         }
-#pragma unroll
-        for (int j = 0; j < VEC; ++j) {
-          if (l.has[n]) mine[l.at0[n] + j] = z0[j];
-          if (l.turns[n]) mine[l.at1[n] + j] = z1[j];
-        }
       }
-      wave_order();
-      double x[16];
+      uint8_t* base = p.mx4.k + h_now * p.mx4.k_sh;
+      if constexpr (ALIGNED) {
+        int e0 = mx4_own_scale(z0[0]), e1 = mx4_own_scale(z1[0]);
+        if (INTERLEAVED) {                         // turning: 16 channels a lane, in two pieces; staying: eight
+          const int both = max(e0, e1), two = pair_max(both), four = four_max(e0);
+          e0 = e1 = l.turns[0] ? two : four;
+        } else {
+          e0 = four_max(e0);
+          e1 = four_max(e1);
+        }
+        if (real && l.has[0]) put(mx4_pack8(z0[0], e0), e0, l.at0[0], t_now, base, 0, p.k_held, h_now);
+        if (real && l.turns[0]) put(mx4_pack8(z1[0], e1), e1, l.at1[0], t_now, base, 0, p.k_held, h_now);
+      } else {
+        wave_order();                              // (a row stays with its lanes, which lie in one wave: LDS keeps a wave's order)
 #pragma unroll
-      for (int j = 0; j < 16; ++j) x[j] = 16 * sub < D ? mine[16 * sub + j] : 0.;
-      put(h0, x, p.mx4.k + page * p.mx4.k_sp + h0 * p.mx4.k_sh, p.k_held);
+        for (int n = 0; n < UPL; ++n)
+#pragma unroll
+          for (int j = 0; j < VEC; ++j) {
+            if (l.has[n]) mine[l.at0[n] + j] = z0[n][j];
+            if (l.turns[n]) mine[l.at1[n] + j] = z1[n][j];
+          }
+        wave_order();
+        double y[16];
+#pragma unroll
+        for (int j = 0; j < 16; ++j) y[j] = 16 * sub < D ? mine[16 * sub + j] : 0.;
+        if (real) put16(y, t_now, base, 0, p.k_held, h_now);
+      }
+    }
+  }
+
+  norm_rows<T, VEC, UPL, INTERLEAVED>(p, l, sub, (const T*)p.q.ptr, p.q.sh, place(0), (T*)p.q_out.ptr, p.q_out.sh, place(1), p.weight[0], p.by_h, q_lo, q_hi, x.cs,
+                                      x.sn);
+
+  if constexpr (MX4) {
+    constexpr int HU = 2;
+    for (int r0 = v_lo + (threadIdx.x >> p.log_lanes); r0 < v_hi; r0 += HU * step) {
+      int t[HU], h[HU];
+      RotaryPiece<T, 8> v0[HU], v1[HU];
+#pragma unroll
+      for (int u = 0; u < HU; ++u) {
+        p.by_hkv.split(min(r0 + u * step, v_hi - 1), t[u], h[u]);
+        const T* row = (const T*)p.v.ptr + x.at[PLACES * t[u] + 3] + h[u] * p.v.sh + (16 * sub < D ? 16 * sub : 0);
+        v0[u] = *(const RotaryPiece<T, 8>*)row;
+        v1[u] = *(const RotaryPiece<T, 8>*)(row + 8);
+      }
+#pragma unroll
+      for (int u = 0; u < HU; ++u) {
+        if (r0 + u * step >= v_hi) break;
+        float y[16];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          y[j] = E::load(v0[u].x[j]);
+          y[8 + j] = E::load(v1[u].x[j]);
+        }
+        put16(y, t[u], p.mx4.v + h[u] * p.mx4.v_sh, 1, p.v_held, h[u]);
+      }
+    }
+  } else {
+    for (int r = v_lo + (threadIdx.x >> p.log_lanes); r < v_hi; r += step) {
+      int t, h;
+      p.by_hkv.split(r, t, h);
+      const int64_t to = x.at[PLACES * t + 5];
+      if (to < 0) continue;
+      const T* in = (const T*)p.v.ptr + x.at[PLACES * t + 3] + h * p.v.sh;
+      T* out = p.v_cache + to + h * p.vc_sh;
+      for (int c = sub * VEC; c < D; c += l.lanes * VEC) *(typename L::Piece*)(out + c) = *(const typename L::Piece*)(in + c);
     }
   }
 }
