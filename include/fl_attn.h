@@ -472,7 +472,7 @@ size_t fl_norm_rotary_bwd_workspace_size(const fl_tensor* q, const fl_tensor* k,
  * A page holds, for each kv head, the codes [page_size][D / 2] (byte i: channel 2 i in bits 0 - 3, 2 i + 1 in bits 4 - 7), then the scales [D / 32][page_size]:
  * page_size * (D / 2 + D / 32) bytes in all, 4.25 bits a value.  D is 64 or 128, page_size a multiple of 8.
  * The fl_tensor of such a cache has dtype FL_MX4, the sizes [pages, 1, Hkv, page_size, D] of the cache it stands for, and in stride[0] and stride[2] the BYTES
- * from page to page and from kv head to kv head (multiples of 16); its other strides are not looked at.
+ * from page to page and from kv head to kv head (multiples of 16, from page to page below 2^32); its other strides are not looked at.
  * What enters is rounded to the nearest code, ties to the even one, under the smallest scale that every magnitude of the block is below 7 of; E is
  * from 1 to 252, so that a held value is finite: infinities become the largest one, NaN zero.  The calls that read expect such E. */
 

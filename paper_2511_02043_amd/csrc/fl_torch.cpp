@@ -908,6 +908,7 @@ PYBIND11_MODULE(_fltorch, m) {
   m.def("paged", &paged, nogil());
   m.def("check_rotary", &check_rotary);
   m.def("check_cache", &check_cache);
+  m.def("check_cache_mx4", &check_cache_mx4);
   m.def("rotary", &rotary, nogil());
   m.def("rotary_checked", &rotary_checked, nogil());
   m.def("rotary_node", &rotary_node, nogil());

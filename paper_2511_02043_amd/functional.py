@@ -643,6 +643,11 @@ def norm_rotary_append(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, positi
     return (out, k_held, v_held) if return_held else out
 
 
+def _check_cache_mx4(q, k_cache, v_cache, seq_lens, block_table, max_seq_len):
+    """Checks the tensors of a 4-bit cache; returns the page size and the host-side bound of the lengths."""
+    return _host().check_cache_mx4(q, k_cache, v_cache, seq_lens, block_table, max_seq_len)
+
+
 def _mx4_call(decode, q, k_cache, v_cache, seq_lens, block_table, max_seq_len, scale, window, softcap, alibi_slopes, workspace, return_lse):
     status, need, out, lse = _host().paged_4bit(decode, q, k_cache, v_cache, seq_lens, block_table, max_seq_len,
                                                 *_paged_variant(q, scale, window, softcap, alibi_slopes), workspace, return_lse, _stream(q))
