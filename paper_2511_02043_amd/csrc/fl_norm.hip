@@ -49,7 +49,7 @@ int tokens_of(const fl::NormParams& p, int64_t workgroups) {
 
 template <class T, int VEC, int UPL>
 hipError_t launch_forward(const fl::NormParams& p, bool il, dim3 grid, hipStream_t stream) {
-  const size_t lds = fl::norm_lds_bytes(p.tokens_per_block, p.pairs, 4);
+  const size_t lds = fl::norm_lds_bytes(p.tokens_per_block, p.pairs, 4, p.D);
   if (il) hipLaunchKernelGGL((fl::norm_rotary_kernel<T, VEC, UPL, true>), grid, dim3(256), lds, stream, p);
   else hipLaunchKernelGGL((fl::norm_rotary_kernel<T, VEC, UPL, false>), grid, dim3(256), lds, stream, p);
   return hipGetLastError();
@@ -63,7 +63,7 @@ hipError_t launch_gradient(const fl::NormParams& p, bool il, dim3 grid, hipStrea
 }
 template <int VEC, int UPL, bool MX4, bool ALIGNED = false>
 hipError_t launch_append(const fl::NormParams& p, bool il, dim3 grid, hipStream_t stream) {
-  size_t lds = fl::norm_lds_bytes(p.tokens_per_block, p.pairs, 9);
+  size_t lds = fl::norm_lds_bytes(p.tokens_per_block, p.pairs, 9, p.D);
   if (MX4) lds += (size_t)p.tokens_per_block * p.pairs * 16;
   if (MX4 && !ALIGNED) lds += (size_t)(256 >> p.log_lanes) * (p.D + 2) * sizeof(double);
   if (il) hipLaunchKernelGGL((fl::norm_append_kernel<VEC, UPL, true, MX4, ALIGNED>), grid, dim3(256), lds, stream, p);

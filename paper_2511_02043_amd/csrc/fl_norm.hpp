@@ -105,8 +105,8 @@ struct NormLane {
     for (int n = 0; n < UPL; ++n)
 #pragma unroll
       for (int j = 0; j < VEC; ++j) {
-        w0[n][j] = w != nullptr ? w[at0[n] + j] : 1.f;
-        w1[n][j] = w != nullptr ? w[at1[n] + j] : 1.f;
+        w0[n][j] = w[at0[n] + j];
+        w1[n][j] = w[at1[n] + j];
       }
   }
   // channels of pair j of a unit: (first piece, element) and (second piece, element)
@@ -217,10 +217,11 @@ __device__ __forceinline__ void norm_rows(const NormParams& p, const NormLane<T,
   }
 }
 
-// A workgroup's LDS: cosines and sines [tokens][pairs], then `places` numbers a token, where its rows begin, then what a kernel has beside.
+// A workgroup's LDS: cosines and sines [tokens][pairs], then `places` numbers a token, where its rows begin, the weights [2][D], then what a kernel has beside.
 struct NormLds {
   float *cs, *sn;
   int64_t* at;
+  float* w;
   void* rest;
 };
 __device__ __forceinline__ NormLds norm_lds(const NormParams& p, void* base, int places) {
@@ -228,10 +229,20 @@ __device__ __forceinline__ NormLds norm_lds(const NormParams& p, void* base, int
   x.cs = (float*)base;
   x.sn = x.cs + p.tokens_per_block * p.pairs;
   x.at = (int64_t*)(x.sn + p.tokens_per_block * p.pairs);
-  x.rest = x.at + places * p.tokens_per_block;
+  x.w = (float*)(x.at + places * p.tokens_per_block);
+  x.rest = x.w + 2 * p.D;
   return x;
 }
-constexpr size_t norm_lds_bytes(int tokens, int pairs, int places) { return (size_t)tokens * (pairs * 8 + places * 8); }
+constexpr size_t norm_lds_bytes(int tokens, int pairs, int places, int D) { return (size_t)tokens * (pairs * 8 + places * 8) + (size_t)D * 8; }
+
+// The weights of queries and keys into LDS.  (Read by every lane from memory when its rows begin, they cost a round trip behind the barrier: 8 x 512 tokens into
+// a bf16 cache 29.6 us, without weights 24.6.)
+__device__ __forceinline__ void hold_weights(const NormParams& p, float* w) {
+  for (int i = threadIdx.x; i < 2 * p.D; i += 256) {
+    const float* from = p.weight[i >= p.D];
+    w[i] = from != nullptr ? from[i < p.D ? i : i - p.D] : 1.f;
+  }
+}
 
 template <class T, int VEC, int UPL, bool INTERLEAVED>
 __global__ void __launch_bounds__(256) norm_rotary_kernel(const NormParams p) {
@@ -248,6 +259,7 @@ __global__ void __launch_bounds__(256) norm_rotary_kernel(const NormParams p) {
     at[2] = row_at(p.k, b, s);
     at[3] = row_at(p.k_out, b, s);
   }
+  hold_weights(p, x.w);
   form_angles<T>(p, token, n, x.cs, x.sn);
   __syncthreads();
   NormLane<T, VEC, UPL, INTERLEAVED> l;
@@ -256,8 +268,8 @@ __global__ void __launch_bounds__(256) norm_rotary_kernel(const NormParams p) {
     norm_rows<T, VEC, UPL, INTERLEAVED>(p, l, sub, (const T*)in.ptr, in.sh, [&](int t) { return x.at[4 * t + place]; }, (T*)out.ptr, out.sh,
                                         [&](int t) { return x.at[4 * t + place + 1]; }, weight, by, 0, n * heads, x.cs, x.sn);
   };
-  rows(p.q, p.q_out, 0, p.H, p.by_h, p.weight[0]);
-  rows(p.k, p.k_out, 2, p.Hkv, p.by_hkv, p.weight[1]);
+  rows(p.q, p.q_out, 0, p.H, p.by_h, x.w);
+  rows(p.k, p.k_out, 2, p.Hkv, p.by_hkv, x.w + p.D);
 }
 
 // The gradient.  Its rows' angles stay in registers: a group of lanes keeps to a token and goes through the chunk of heads that the workgroup has of it, the next
@@ -269,7 +281,7 @@ template <class T, int VEC, int UPL, bool INTERLEAVED>
 __global__ void __launch_bounds__(256) norm_rotary_bwd_kernel(const NormParams p) {
   typedef NormLane<T, VEC, UPL, INTERLEAVED> L;
   typedef RotaryElem<T> E;
-  extern __shared__ float dw_lds[];                // [waves][D]
+  extern __shared__ float dw_lds[];                // [waves][D]; before, the weights
   const int sub = threadIdx.x & ((1 << p.log_lanes) - 1), local = threadIdx.x >> p.log_lanes;
   L l;
   l.init(p, sub);
@@ -277,7 +289,10 @@ __global__ void __launch_bounds__(256) norm_rotary_bwd_kernel(const NormParams p
   const int heads = keys ? p.Hkv : p.H, h_begin = (blockIdx.y - (keys ? p.q_chunks : 0)) * p.heads_per_thread, h_end = min(h_begin + p.heads_per_thread, heads);
   const View &xv = keys ? p.k : p.q, &yv = p.dy[keys], &ov = p.dx[keys];
   float w0[UPL][VEC], w1[UPL][VEC], d0[UPL][VEC] = {}, d1[UPL][VEC] = {};
-  l.weights(p.weight[keys], w0, w1);
+  for (int i = threadIdx.x; i < p.D; i += 256) dw_lds[i] = p.weight[keys] != nullptr ? p.weight[keys][i] : 1.f;
+  __syncthreads();
+  l.weights(dw_lds, w0, w1);
+  __syncthreads();                                 // (before anyone's sums take their place)
   const float inv_d = 1.f / p.D;
 
   for (int group = blockIdx.x; group < p.groups; group += p.blocks) {
@@ -285,6 +300,12 @@ __global__ void __launch_bounds__(256) norm_rotary_bwd_kernel(const NormParams p
     if (token >= (int64_t)p.B * p.S) continue;     // (whole groups of lanes)
     int b, s;
     p.by_s.split((int)token, b, s);
+    const T* x_in = (const T*)xv.ptr + row_at(xv, b, s);
+    const T* y_in = (const T*)yv.ptr + row_at(yv, b, s);
+    T* out = (T*)ov.ptr + row_at(ov, b, s);
+    typename L::Piece x0[UPL], x1[UPL], y0[UPL], y1[UPL];
+    l.load(x_in + h_begin * xv.sh, x0, x1);
+    l.load(y_in + h_begin * yv.sh, y0, y1);
     float cs[UPL][VEC], sn[UPL][VEC];
 #pragma unroll
     for (int n = 0; n < UPL; ++n)
@@ -294,12 +315,6 @@ __global__ void __launch_bounds__(256) norm_rotary_bwd_kernel(const NormParams p
         sn[n][j] = 0.f;
         if (l.turns[n]) E::sincos_turns((float)turn_of(p, (int)token, (sub + n * l.lanes) * VEC + j), sn[n][j], cs[n][j]);
       }
-    const T* x_in = (const T*)xv.ptr + row_at(xv, b, s);
-    const T* y_in = (const T*)yv.ptr + row_at(yv, b, s);
-    T* out = (T*)ov.ptr + row_at(ov, b, s);
-    typename L::Piece x0[UPL], x1[UPL], y0[UPL], y1[UPL];
-    l.load(x_in + h_begin * xv.sh, x0, x1);
-    l.load(y_in + h_begin * yv.sh, y0, y1);
     for (int h = h_begin; h < h_end; ++h) {
       float sum[2] = {};                           // of x^2 and of x g
       float z0[UPL][VEC], z1[UPL][VEC], a0[UPL][VEC], a1[UPL][VEC];                  // dz, x
@@ -412,6 +427,7 @@ __global__ void __launch_bounds__(256) norm_append_kernel(const NormParams p) {
   double* const sn64 = cs64 + p.tokens_per_block * p.pairs;
   const int sub = threadIdx.x & ((1 << p.log_lanes) - 1), step = 256 >> p.log_lanes;
   const int token = blockIdx.x * p.tokens_per_block, n = min(p.tokens_per_block, p.B * p.S - token);
+  const int D = p.D;
   // this workgroup's keys [lo, hi), queries and values
   const int part = blockIdx.y * p.rows_per_part, part_end = part + p.rows_per_part, n_k = n * p.Hkv, n_q = n * p.H;
   auto cut = [&](int first, int rows, int& lo, int& hi) __attribute__((always_inline)) {
@@ -450,6 +466,7 @@ __global__ void __launch_bounds__(256) norm_append_kernel(const NormParams p) {
     at[5] = page < 0 ? -1 : (MX4 ? page * p.mx4.v_sp : page * p.vc_sp + within * p.vc_st);
     at[6] = within;
   }
+  if (q_lo < q_hi || k_lo < k_hi) hold_weights(p, x.w);
   if (q_lo < q_hi || (!MX4 && k_lo < k_hi)) form_angles<T>(p, token, n, x.cs, x.sn);
   if (MX4 && k_lo < k_hi) {
     for (int i = threadIdx.x; i < n * p.pairs; i += 256) {
@@ -467,7 +484,6 @@ __global__ void __launch_bounds__(256) norm_append_kernel(const NormParams p) {
   auto place = [&](int i) __attribute__((always_inline)) { return [=](int t) { return x.at[PLACES * t + i]; }; };
 
   // Eight channels of a row of token t from channel `at` on under the block's scale byte e: to the page (base: of the head) and to the caller
-  const int D = p.D;
   auto put = [&](uint32_t codes, int e, int at, int t, uint8_t* base, int which, const View& held, int head) __attribute__((always_inline)) {
     const int64_t page = x.at[PLACES * t + 4 + which], within = x.at[PLACES * t + 6];
     if (page >= 0) {
@@ -486,10 +502,10 @@ __global__ void __launch_bounds__(256) norm_append_kernel(const NormParams p) {
   };
 
   if constexpr (!MX4) {
-    norm_rows<T, VEC, UPL, INTERLEAVED>(p, l, sub, (const T*)p.k.ptr, p.k.sh, place(2), p.k_cache, p.kc_sh, place(4), p.weight[1], p.by_hkv, k_lo, k_hi, x.cs, x.sn);
+    norm_rows<T, VEC, UPL, INTERLEAVED>(p, l, sub, (const T*)p.k.ptr, p.k.sh, place(2), p.k_cache, p.kc_sh, place(4), x.w + D, p.by_hkv, k_lo, k_hi, x.cs, x.sn);
   } else if (k_lo < k_hi) {
     float w0[UPL][VEC], w1[UPL][VEC];
-    l.weights(p.weight[1], w0, w1);
+    l.weights(x.w + D, w0, w1);
     double* const mine = sn64 + p.tokens_per_block * p.pairs + (threadIdx.x >> p.log_lanes) * (D + 2);     // not ALIGNED: a row of this group of lanes
     typename L::Piece x0[UPL], x1[UPL];
     int t, h;
@@ -560,7 +576,7 @@ __global__ void __launch_bounds__(256) norm_append_kernel(const NormParams p) {
     }
   }
 
-  norm_rows<T, VEC, UPL, INTERLEAVED>(p, l, sub, (const T*)p.q.ptr, p.q.sh, place(0), (T*)p.q_out.ptr, p.q_out.sh, place(1), p.weight[0], p.by_h, q_lo, q_hi, x.cs,
+  norm_rows<T, VEC, UPL, INTERLEAVED>(p, l, sub, (const T*)p.q.ptr, p.q.sh, place(0), (T*)p.q_out.ptr, p.q_out.sh, place(1), x.w, p.by_h, q_lo, q_hi, x.cs,
                                       x.sn);
 
   if constexpr (MX4) {
