@@ -493,16 +493,18 @@ fl_status fl_norm_rotary_append(const fl_tensor* q, const fl_tensor* k, const fl
 fl_status fl_attn_decode_mx4(const fl_tensor* q, const fl_tensor* k_cache, const fl_tensor* v_cache, const fl_paged_kv* kv, const fl_variant_desc* desc,
                              const fl_aux* aux, fl_tensor* out, fl_tensor* lse, void* stream);
 
-/* Bytes of aux->workspace that fl_attn_decode_mx4 needs. */
+/* Bytes of aux->workspace that fl_attn_decode_mx4 needs; 0 where no sequence is split among workgroups: the workspace may then be NULL. */
 size_t fl_attn_decode_mx4_workspace_size(const fl_tensor* q, const fl_tensor* k_cache, const fl_paged_kv* kv);
 
-/* fl_attn_prefill_paged over a 4-bit cache (D 64 or 128).  Chunks of so few rows that Sq * H / Hkv <= 64 are an fl_attn_decode_mx4 call; otherwise the
- * sequences' keys and values are unpacked to dense bf16 tensors in the workspace, which the forward kernel then reads. */
+/* fl_attn_prefill_paged over a 4-bit cache (D 64 or 128).  Chunks of few rows go through the kernels of fl_attn_decode_mx4, some of their rows at a time;
+ * where that takes longer, by an estimate from the sizes, the sequences' keys and values are unpacked to dense bf16 tensors in the workspace, which
+ * the forward kernel then reads. */
 fl_status fl_attn_prefill_mx4(const fl_tensor* q, const fl_tensor* k_cache, const fl_tensor* v_cache, const fl_paged_kv* kv, const fl_variant_desc* desc,
                               const fl_aux* aux, fl_tensor* out, fl_tensor* lse, void* stream);
 
-/* Bytes of aux->workspace that fl_attn_prefill_mx4 needs: fl_attn_decode_mx4_workspace_size for chunks of a few rows, else the dense
- * copies, 2 * B * Hkv * max_seq_len * D * 2 bytes (each rounded up to 256). */
+/* Bytes of aux->workspace that fl_attn_prefill_mx4 needs under any mask: fl_attn_decode_mx4_workspace_size where Sq * H / Hkv <= 64, else the larger of
+ * that (up to Sq * H / Hkv = 16384) and the dense copies, 2 * B * Hkv * max_seq_len * D * 2 bytes (each rounded up to 256).  A call that goes the way which
+ * needs less takes less. */
 size_t fl_attn_prefill_mx4_workspace_size(const fl_tensor* q, const fl_tensor* k_cache, const fl_paged_kv* kv);
 
 /* A variant compiled at run time from user expressions (opaque; owned by the caller until released). */
@@ -614,7 +616,7 @@ const char* fl_last_error_detail(void);
  * 2 = a long and a short q-tile per workgroup), "decode_splits" (key-range splits per sequence and
  * kv head of fl_attn_decode and fl_attn_decode_mx4), "bwd_wg_target" (workgroups up to which fl_attn_bwd cuts a group of
  * query heads into subsets; both change the workspace size the matching *_workspace_size reports),
- * "prefill_gather" (fl_attn_prefill_paged: 1 = always copy the pages first, 2 = always read them in place with the
+ * "prefill_gather" (fl_attn_prefill_paged and, but for 2, fl_attn_prefill_mx4: 1 = always copy the pages first, 2 = always read them in place with the
  * forward kernel; either also keeps chunks of a few rows away from the decode kernels), "prefill_pack" (1 = never
  * pack the query heads of a kv head into one workgroup of the in-place kernel), "bwd_keys" (the dK / dV kernel with 64 keys per wave:
  * 1 = never, 2 = always where the variant has one), "pair_bias" (fl_attn_bwd_ex with a bias shared

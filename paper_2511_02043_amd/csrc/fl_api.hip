@@ -2615,3 +2615,4 @@ fl_status fl::host::forward_of_lengths(const fl_tensor* q, const fl_tensor* k, c
 }
 
 int fl::host::tuned_decode_splits() { return g_tuning.decode_splits; }
+int fl::host::tuned_prefill_gather() { return g_tuning.prefill_gather; }

@@ -244,8 +244,9 @@ inline fl_status check_cache_mx4(const fl_paged_kv* kv, const fl_tensor* k_cache
 fl_status forward_of_lengths(const fl_tensor* q, const fl_tensor* k, const fl_tensor* v, const fl_variant_desc* desc, const fl_aux* aux, fl_tensor* out,
                              fl_tensor* lse, void* stream, const int32_t* kv_lens);
 
-// What fl_set_tuning("decode_splits") asks for in this thread; 0: nothing.
+// What fl_set_tuning("decode_splits") and fl_set_tuning("prefill_gather") ask for in this thread; 0: nothing.
 int tuned_decode_splits();
+int tuned_prefill_gather();
 
 }  // namespace host
 }  // namespace fl

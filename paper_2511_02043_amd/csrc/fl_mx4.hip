@@ -11,17 +11,61 @@ namespace {
 
 using namespace fl::host;
 
-constexpr int64_t kMostPairs = 64;                 // (query row, head) pairs of a kv head: four column blocks of 16
+constexpr int64_t kMostPairs = 64;                 // (query row, head) pairs of a kv head that a decode step takes
+constexpr int64_t kMostRowPairs = 16384;           // ... that a chunk may bring through the decode kernels
 
-// Splits of a sequence's keys, from the shapes and the host-side bound of the lengths alone.
-int splits_of(int64_t B, int64_t Hkv, int64_t max_seq_len) {
-  const int64_t tiles = (max_seq_len + 31) / 32, units = std::max<int64_t>(1, B * Hkv);
-  if (tuned_decode_splits() > 0) return (int)std::max<int64_t>(1, std::min<int64_t>(tuned_decode_splits(), tiles));
-  const int64_t want = std::min<int64_t>({(512 + units - 1) / units, tiles / 4, 64});
-  return (int)std::max<int64_t>(1, want);
+int64_t pairs_of(int64_t H, int64_t Hkv, int64_t T) { return Hkv > 0 && T <= kMostRowPairs ? T * (H / Hkv) : kMostRowPairs + 1; }
+// Blocks of pairs, each a workgroup's: 16 of them, where there are more 32 (16 rows of 8 sequences of 4k - 8k tokens, 32 / 8 heads, D = 128: 36 us in two blocks; 59 in one of
+// 64, whose registers leave room for one wave per SIMD).
+int64_t blocks_of(int64_t pairs) { return pairs <= 16 ? 1 : (pairs + 31) / 32; }
+
+// Keys that the rows of one or all blocks see at most, `rows` of them under this mask.
+int64_t keys_of(const fl_variant_desc* desc, int64_t max_seq_len, int64_t rows) {
+  const bool window = canonical_mask(desc->mask) & FL_MASK_WINDOW;
+  return window ? std::min<int64_t>(max_seq_len, clamp_window(desc->window, max_seq_len, max_seq_len) + rows) : max_seq_len;
 }
 
-size_t decode_bytes(int64_t B, int64_t T, int64_t H, int64_t D, int ns) { return (size_t)(B * T * H * ns) * (size_t)(D + 2) * sizeof(float); }
+// Splits of a sequence's keys, from the shapes, the host-side bound of the lengths and the most keys that a sequence's rows see: the power of two that
+// brings the workgroups to 448 or more, or fewer where a shorter chain of tiles (0.65 us each, of 32 pairs 0.9) does not pay for the merge (3 us, and 1.6 ns and 0.3 a split
+// for each row).  us, 32 / 8 heads, D = 128, splits: 64 sequences of 4k - 8k tokens 1: 87.7, 2: 89.9; 24 of them 1: 45.9, 2: 38.0, 4: 35.7, 8: 38; 8 of them 1: 43,
+// 4: 17.8, 8: 16.9, 16: 18.0; 2 of 100k - 131k 16: 51.9, 32: 52.4, 64: 55.4; 48 of 512 - 1024 1: 12.5, 2: 15.2; eight rows of 24 of 1k - 2k 1: 20.0, 2: 23.8, 3: 28.3.
+// Never more for fewer keys: a workspace that was sized without the window is large enough.
+int splits_of(int64_t B, int64_t H, int64_t Hkv, int64_t T, int64_t keys) {
+  const int64_t tiles = (keys + 31) / 32, pairs = pairs_of(H, Hkv, T), units = std::max<int64_t>(1, B * Hkv * blocks_of(pairs));
+  if (tuned_decode_splits() > 0) return (int)std::max<int64_t>(1, std::min<int64_t>(tuned_decode_splits(), tiles));
+  const double chain = (pairs <= 16 ? 0.65 : 0.9) * (double)tiles / 4, rows = (double)B * (double)T * (double)H;
+  int best = 1;
+  double least = chain;
+  for (int ns = 2; ns <= 64 && ns * 4 <= tiles && units * (ns / 2) < 448; ns *= 2) {
+    const double us = chain / ns + 3 + rows * (1.6e-3 + 3e-4 * ns);
+    if (us < least) least = us, best = ns;
+  }
+  return best;
+}
+
+// Partial results; a sequence that is not split has none.
+size_t decode_bytes(int64_t B, int64_t T, int64_t H, int64_t D, int ns) { return ns > 1 ? (size_t)(B * T * H * ns) * (size_t)(D + 2) * sizeof(float) : 0; }
+
+size_t dense_bytes(int64_t B, int64_t Hkv, int64_t D, int64_t max_len) {
+  return ((size_t)(B * Hkv * std::max<int64_t>(max_len, 1) * D) * 2 + 255) / 256 * 256;
+}
+
+// Whether a chunk's rows go through the decode kernels, 32 pairs of a kv head at a time, or its sequences are unpacked for the forward kernel.  The former read the keys
+// again for each 32 pairs (52 000 keys of such a block a microsecond at D = 128, 72 000 at 64, and 256 keys' time to start); the latter have the unpacking, then a tile's chain over
+// the keys or, if that is longer, their products.  us, rows / unpacked, T = 16, 64, 128, 256, 512 rows: 8 sequences of 4k - 8k tokens, 32 / 8 heads, D = 128 36 / 186, 91 / 235,
+// 162 / 189, 311 / 250, 596 / 428; one of 8k 17 / 148, 25 / 199, 35 / 144, 56 / 144, 88 / 149; 16 of 500 - 1000 24 / 47, 31 / 48, 55 / 53, 99 / 78; 4 of 700 - 1500, 16 / 2 heads,
+// D = 64, window 512 12 / 22, 14 / 24, 16 / 25, 12 / 25, 20 / 26.
+bool through_decode(int64_t B, int64_t H, int64_t Hkv, int64_t T, int64_t D, int64_t max_len, const fl_variant_desc* desc) {
+  const int64_t pairs = pairs_of(H, Hkv, T);
+  if (pairs > kMostRowPairs || tuned_prefill_gather() == 1) return false;
+  if (pairs <= kMostPairs) return true;
+  const double wide = D == 128 ? 1. : 0., ahead = (double)std::max<int64_t>(0, max_len - T / 2);     // (rows of a prompt see half of it)
+  const double rows_us = 10 + (double)(B * Hkv * blocks_of(pairs)) * (std::min(ahead, (double)keys_of(desc, max_len, 32)) + 256) / (wide ? 52e3 : 72e3);
+  const double chain = (double)keys_of(desc, max_len, T) * (wide ? 0.0145 : 0.0112);
+  const double products = 4. * (double)(B * H) * (double)T * std::min(ahead, (double)keys_of(desc, max_len, 0)) * (double)D / (wide ? 1.45e9 : 1.15e9);
+  const double unpacked_us = 16 + (double)(B * Hkv) * (double)(max_len * D) * 7.2e-7 + std::max(chain, products);
+  return rows_us <= unpacked_us;
+}
 
 template <int D, int MOD, int NB>
 hipError_t launch_blocks(const fl::Mx4DecodeParams& p, int blocks, hipStream_t stream) {
@@ -32,7 +76,7 @@ hipError_t launch_blocks(const fl::Mx4DecodeParams& p, int blocks, hipStream_t s
 }
 template <int D, int MOD>
 hipError_t launch_decode(const fl::Mx4DecodeParams& p, int blocks, int pairs, hipStream_t stream) {
-  return pairs <= 16 ? launch_blocks<D, MOD, 1>(p, blocks, stream) : (pairs <= 32 ? launch_blocks<D, MOD, 2>(p, blocks, stream) : launch_blocks<D, MOD, 4>(p, blocks, stream));
+  return pairs <= 16 ? launch_blocks<D, MOD, 1>(p, blocks, stream) : launch_blocks<D, MOD, 2>(p, blocks, stream);
 }
 template <int D>
 hipError_t launch_decode(uint32_t mod, const fl::Mx4DecodeParams& p, int blocks, int pairs, hipStream_t stream) {
@@ -83,6 +127,7 @@ fl_status check_call(const char* name, const fl_tensor* q, const fl_tensor* k_ca
 }
 
 fl_status check_workspace(const fl_aux* aux, size_t need) {
+  if (need == 0) return FL_OK;
   if (aux->workspace == nullptr || aux->workspace_bytes < need)
     return fail(FL_ERR_WORKSPACE, "workspace needs %zu bytes, got %zu", need, aux->workspace ? aux->workspace_bytes : (size_t)0);
   if (((uintptr_t)aux->workspace) % 16 != 0) return fail(FL_ERR_ALIGN, "workspace not 16-byte aligned");
@@ -93,10 +138,11 @@ fl_status check_workspace(const fl_aux* aux, size_t need) {
 fl_status decode(const fl_tensor* q, const fl_tensor* k_cache, const fl_tensor* v_cache, const fl_paged_kv* kv, const fl_variant_desc* desc, const fl_aux* aux,
                  fl_tensor* out, fl_tensor* lse, int page_shift, hipStream_t stream) {
   const int64_t B = q->size[0], H = q->size[2], T = q->size[3], D = q->size[4], Hkv = k_cache->size[2];
-  const int ns = splits_of(B, Hkv, kv->max_seq_len);
+  const int ns = splits_of(B, H, Hkv, T, keys_of(desc, kv->max_seq_len, T));
   const fl_status st = check_workspace(aux, decode_bytes(B, T, H, D, ns));
   if (st != FL_OK) return st;
-  if (B * Hkv * ns > 0x7fffffffLL || B * T * H > 0x7fffffffLL) return fail(FL_ERR_SHAPE, "too many workgroups");
+  const int64_t row_blocks = blocks_of(pairs_of(H, Hkv, T));
+  if (B * Hkv * ns * row_blocks > 0x7fffffffLL || B * T * H > 0x7fffffffLL) return fail(FL_ERR_SHAPE, "too many workgroups");
   const uint32_t mask = canonical_mask(desc->mask);
   fl::Mx4DecodeParams p;
   memset(&p, 0, sizeof(p));
@@ -124,6 +170,7 @@ fl_status decode(const fl_tensor* q, const fl_tensor* k_cache, const fl_tensor* 
   p.B = (int)B; p.H = (int)H; p.Hkv = (int)Hkv; p.T = (int)T;
   p.nsplit = ns;
   p.by_split = fl::Divisor::of(ns);
+  p.by_block = fl::Divisor::of(row_blocks);
   p.by_hkv = fl::Divisor::of(Hkv);
   p.by_group = fl::Divisor::of(H / Hkv);
   p.by_h = fl::Divisor::of(H);
@@ -131,15 +178,9 @@ fl_status decode(const fl_tensor* q, const fl_tensor* k_cache, const fl_tensor* 
   p.window = (mask & FL_MASK_WINDOW) ? clamp_window(desc->window, kv->max_seq_len, kv->max_seq_len) : -1;
   p.scale = desc->scale;
   p.softcap = std::fmin(std::fmax(desc->softcap, 0x1p-120f), 0x1p120f);   // (both and twice them finite; beyond them every score is 0 in fp32, as at them)
-  const int blocks = (int)(B * Hkv * ns), pairs = (int)(T * (H / Hkv));
+  const int blocks = (int)(B * Hkv * ns * row_blocks), pairs = (int)(T * (H / Hkv));
   const hipError_t e = D == 128 ? launch_decode<128>(desc->score_mod, p, blocks, pairs, stream) : launch_decode<64>(desc->score_mod, p, blocks, pairs, stream);
   return e == hipSuccess ? FL_OK : fail(FL_ERR_LAUNCH, "decode launch: %s", hipGetErrorString(e));
-}
-
-bool few_rows(int64_t H, int64_t Hkv, int64_t Sq) { return Hkv > 0 && Sq <= kMostPairs && Sq * (H / Hkv) <= kMostPairs; }
-
-size_t dense_bytes(int64_t B, int64_t Hkv, int64_t D, int64_t max_len) {
-  return ((size_t)(B * Hkv * std::max<int64_t>(max_len, 1) * D) * 2 + 255) / 256 * 256;
 }
 
 }  // namespace
@@ -148,7 +189,8 @@ extern "C" {
 
 size_t fl_attn_decode_mx4_workspace_size(const fl_tensor* q, const fl_tensor* k_cache, const fl_paged_kv* kv) {
   if (q == nullptr || k_cache == nullptr || kv == nullptr) return 0;
-  return decode_bytes(q->size[0], q->size[3], q->size[2], q->size[4], splits_of(q->size[0], k_cache->size[2], kv->max_seq_len));
+  const int64_t B = q->size[0], H = q->size[2], T = q->size[3];
+  return decode_bytes(B, T, H, q->size[4], splits_of(B, H, k_cache->size[2], T, kv->max_seq_len));
 }
 
 fl_status fl_attn_decode_mx4(const fl_tensor* q, const fl_tensor* k_cache, const fl_tensor* v_cache, const fl_paged_kv* kv, const fl_variant_desc* desc,
@@ -158,7 +200,7 @@ fl_status fl_attn_decode_mx4(const fl_tensor* q, const fl_tensor* k_cache, const
   bool empty = false;
   const fl_status st = check_call("the decode step over 4 bits", q, k_cache, v_cache, kv, desc, aux, out, lse, &page_shift, &empty);
   if (st != FL_OK) return st;
-  if (q->size[2] != 0 && !few_rows(q->size[2], k_cache->size[2], q->size[3]))
+  if (q->size[2] != 0 && pairs_of(q->size[2], k_cache->size[2], q->size[3]) > kMostPairs)
     return fail(FL_ERR_SHAPE, "at most %lld (query row, q head) pairs per kv head (T = %lld)", (long long)kMostPairs, (long long)q->size[3]);
   if (empty) return FL_OK;
   return decode(q, k_cache, v_cache, kv, desc, aux, out, lse, page_shift, (hipStream_t)stream);
@@ -166,8 +208,9 @@ fl_status fl_attn_decode_mx4(const fl_tensor* q, const fl_tensor* k_cache, const
 
 size_t fl_attn_prefill_mx4_workspace_size(const fl_tensor* q, const fl_tensor* k_cache, const fl_paged_kv* kv) {
   if (q == nullptr || k_cache == nullptr || kv == nullptr) return 0;
-  if (few_rows(q->size[2], k_cache->size[2], q->size[3])) return fl_attn_decode_mx4_workspace_size(q, k_cache, kv);
-  return 2 * dense_bytes(q->size[0], k_cache->size[2], q->size[4], kv->max_seq_len);
+  const int64_t pairs = pairs_of(q->size[2], k_cache->size[2], q->size[3]);
+  const size_t split = pairs <= kMostRowPairs ? fl_attn_decode_mx4_workspace_size(q, k_cache, kv) : 0;
+  return pairs <= kMostPairs && tuned_prefill_gather() != 1 ? split : std::max(split, 2 * dense_bytes(q->size[0], k_cache->size[2], q->size[4], kv->max_seq_len));
 }
 
 fl_status fl_attn_prefill_mx4(const fl_tensor* q, const fl_tensor* k_cache, const fl_tensor* v_cache, const fl_paged_kv* kv, const fl_variant_desc* desc,
@@ -179,7 +222,7 @@ fl_status fl_attn_prefill_mx4(const fl_tensor* q, const fl_tensor* k_cache, cons
   if (st != FL_OK || empty) return st;
   hipStream_t stream = (hipStream_t)stream_v;
   const int64_t B = q->size[0], H = q->size[2], Sq = q->size[3], D = q->size[4], Hkv = k_cache->size[2], L = kv->max_seq_len;
-  if (few_rows(H, Hkv, Sq)) return decode(q, k_cache, v_cache, kv, desc, aux, out, lse, page_shift, stream);
+  if (through_decode(B, H, Hkv, Sq, D, L, desc)) return decode(q, k_cache, v_cache, kv, desc, aux, out, lse, page_shift, stream);
 
   // the inner forward call: causal, every sequence's key count read on the device.  What it can refuse is checked before the first launch.
   fl_variant_desc inner = *desc;

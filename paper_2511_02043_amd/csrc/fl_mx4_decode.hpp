@@ -60,6 +60,7 @@ __global__ void __launch_bounds__(256) mx4_unpack_kernel(const Mx4UnpackParams p
 
 struct Mx4DecodeParams : DecodeParams {
   Mx4Cache cache;                  // in place of k, v and their strides
+  Divisor by_block;                // blocks of 16 NB (query row, head) pairs of a kv head
 };
 
 // max and sum over the four lanes of a column (16 apart)
@@ -80,7 +81,7 @@ __device__ __forceinline__ float quarter_sum(float x) {
 //   * for that one, a lane has keys 8 g .. + 7 of channels D/16 m .. + D/16 - 1: the codes of two keys are converted two channels at a time, then
 //     paired key by key.
 // Waves of a SIMD, which are workgroups of a compute unit: what the registers of an instance leave room for.  LDS is shared out among them as rings.
-constexpr int mx4_decode_waves(int D, int NB) { return NB == 1 ? 4 : (NB == 2 ? 2 : 1); }
+constexpr int mx4_decode_waves(int D, int NB) { return NB == 1 ? 4 : 2; }
 template <int D, int NB>
 struct Mx4Ring {
   static constexpr int V = 32 * (D / 2), E = 2 * V, STAGE = E + 256;             // bytes: keys, values, scales
@@ -107,22 +108,24 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(mx4_de
   // workgroups go out to the eight XCDs in turn: an XCD takes neighbours, whose kv heads share the lines of memory in which one's part of a page ends and
   // the next one's begins (64 sequences of 4k - 8k tokens, 32 / 8 heads, D = 128: 87.7 -> 86.5 us)
   const int place = (gridDim.x & 7) == 0 ? (int)((blockIdx.x & 7) * (gridDim.x >> 3) + (blockIdx.x >> 3)) : (int)blockIdx.x;
-  int split, bhk, hk, b;
-  p.by_split.split(place, bhk, split);
+  int rest, block, split, bhk, hk, b;
+  p.by_block.split(place, rest, block);            // blocks of a split's rows side by side: they read the same keys
+  p.by_split.split(rest, bhk, split);
   p.by_hkv.split(bhk, b, hk);
-  const int len = min(max(p.seq_lens[b], 0), p.max_len);
-  const int t_lo = p.window >= 0 ? max(0, len - p.T - p.window) / 32 : 0, t_hi = (len + 31) / 32;
-  const int per_split = p.by_split.div(t_hi - t_lo + p.nsplit - 1);   // (a sequence without tiles: t_lo <= t_hi all the same)
+  const int len = min(max(p.seq_lens[b], 0), p.max_len), first_pair = block * 16 * NB, last_pair = min(first_pair + 16 * NB, ncol) - 1;
+  const int pos_lo = len - p.T + p.by_group.div(first_pair), pos_hi = len - p.T + p.by_group.div(last_pair);     // of the first and last row
+  const int t_lo = p.window >= 0 ? max(0, pos_lo - p.window) / 32 : 0, t_hi = pos_hi < 0 ? 0 : pos_hi / 32 + 1;
+  const int per_split = p.by_split.div(max(t_hi - t_lo, 0) + p.nsplit - 1);
   const int t_begin = t_lo + split * per_split, t_end = min(t_hi, t_begin + per_split);
   int row[NB], hq[NB], pos[NB];                    // (columns behind the last pair are copies of it)
 #pragma unroll
   for (int nb = 0; nb < NB; ++nb) {
     int head;
-    p.by_group.split(min(16 * nb + m, ncol - 1), row[nb], head);
+    p.by_group.split(min(first_pair + 16 * nb + m, last_pair), row[nb], head);
     hq[nb] = hk * group + head;
     pos[nb] = len - p.T + row[nb];
   }
-  const int first_full = p.window >= 0 ? max(0, len - 1 - p.window) : 0;
+  const int first_full = p.window >= 0 ? max(0, pos_hi - p.window) : 0;
 
   bf16x8 qf[NB][KS];
   float slope2[NB], m_run[NB], l_run[NB];
@@ -236,7 +239,7 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(mx4_de
       }
     }
     const int jb = t * 32 + 8 * g;
-    const bool partial = t * 32 + 32 > len - p.T + 1 || t * 32 < first_full;       // uniform
+    const bool partial = t * 32 + 32 > pos_lo + 1 || t * 32 < first_full;       // uniform
     bf16x8 pf[NB];
 #pragma unroll
     for (int nb = 0; nb < NB; ++nb) {
@@ -379,7 +382,7 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(mx4_de
       for (int u = 0; u < 4; ++u) x[k] = fmaf(park(u)[(k * 4 + wave) * 64 + lane], wgt[u], x[k]);
       x[k] *= inv;
     }
-    if (16 * nb + m >= ncol) continue;
+    if (first_pair + 16 * nb + m > last_pair) continue;
     const int64_t slot = (((int64_t)b * p.T + row[nb]) * p.H + hq[nb]) * p.nsplit + split;
     const int ch = CH * (4 * g + wave);
     if (!result || p.out_f32) {

@@ -283,14 +283,50 @@ def test_decode_of_one_long_sequence_and_of_many_short_ones():
         assert same(out, again[0]) and same(lse, again[1])
 
 
+@pytest.fixture(params=["rows", "unpacked"])
+def way(request):
+    """Chunks as the library sends them (all that are here: through the decode kernels), and unpacked for the forward kernel."""
+    fb.check(fb.fl_set_tuning("prefill_gather", 0 if request.param == "rows" else 1))
+    yield request.param
+    fb.check(fb.fl_set_tuning("prefill_gather", 0))
+
+
 @pytest.mark.parametrize("name", VARIANTS)
 @pytest.mark.parametrize("D,page,H,Hkv,Sq,lens", [(128, 16, 4, 2, 40, [40, 100, 7]), (64, 8, 2, 2, 77, [200, 77]), (128, 64, 8, 1, 9, [9, 60]), (64, 16, 2, 1, 130, [131, 0, 129]),
-                                                  (128, 8, 4, 4, 12, [300])])
-def test_prefill(D, page, H, Hkv, Sq, lens, name):
+                                                  (128, 8, 4, 4, 12, [300]), (64, 32, 6, 2, 33, [33, 1000, 34, 32, 1]), (128, 16, 16, 2, 45, [700, 44])])
+def test_prefill(D, page, H, Hkv, Sq, lens, name, way):
     B = len(lens)
     kc, vc, table = pool(B, Hkv, D, page, -(-max(lens) // page))
     q = torch.randn(B, H, Sq, D, generator=torch.Generator().manual_seed(2)).bfloat16().cuda()
     attend(F.paged_prefill_attention_mx4, q, kc, vc, lens, table, page, name)
+
+
+@pytest.mark.parametrize("name", VARIANTS)
+@pytest.mark.parametrize("D", [64, 128])
+def test_a_chunk_whose_rows_are_split_among_workgroups(D, name):
+    """Blocks of rows whose keys end, and under a window begin, in other tiles than the chunk's."""
+    lens, page, H, Hkv, Sq = [2500, 2049, 70], 16, 6, 2, 50
+    kc, vc, table = pool(3, Hkv, D, page, -(-max(lens) // page))
+    q = torch.randn(3, H, Sq, D, generator=torch.Generator().manual_seed(3)).bfloat16().cuda()
+    for splits in (0, 1, 5, 64):
+        fb.check(fb.fl_set_tuning("decode_splits", splits))
+        try:
+            attend(F.paged_prefill_attention_mx4, q, kc, vc, lens, table, page, name)
+        finally:
+            fb.check(fb.fl_set_tuning("decode_splits", 0))
+
+
+def test_many_rows_of_long_prompts():
+    """Prompts that the library unpacks by itself, on some of their rows: those of a chunk that ends there."""
+    B, H, Hkv, D, page, n = 2, 16, 2, 64, 16, 3000
+    kc, vc, table = pool(B, Hkv, D, page, -(-n // page))
+    q = torch.randn(B, H, n, D, generator=torch.Generator().manual_seed(4)).bfloat16().cuda()
+    scale = 0.3 * D ** -0.5
+    out, lse = F.paged_prefill_attention_mx4(q, kc, vc, ints([n, n - 7]), table, scale=scale, return_lse=True)
+    for first, rows in ((0, 40), (1500, 9), (2990, 10)):
+        end = first + rows
+        check_attention(out[:, :, first:end], lse[:, :, first:end], q[:, :, first:end], kc, vc, [end, end - 7], table, page, scale=scale)
+    assert not out[1, :, :7].any() and bool(torch.isneginf(lse[1, :, :7]).all())
 
 
 def test_without_a_table_and_with_other_strides():
@@ -401,15 +437,16 @@ def test_far_pages():
 
 
 def test_fp32_results_and_workspaces_through_the_abi():
-    B, H, Hkv, D, page, lens = 2, 8, 2, 128, 16, [900, 33]
-    kc, vc, table = pool(B, Hkv, D, page, 60)
+    B, H, Hkv, D, page, lens = 2, 8, 2, 128, 16, [6000, 33]
+    kc, vc, table = pool(B, Hkv, D, page, 400)
     q = torch.randn(B, H, 1, D, device="cuda").bfloat16()
     want, want_lse = F.decode_attention_mx4(q[:, :, 0], kc, vc, ints(lens), table, return_lse=True)
     out, lse = torch.zeros(B, H, 1, D, device="cuda"), torch.zeros(B, H, 1, 1, device="cuda")
     seq = ints(lens)
-    kv = fb.paged_kv(block_table=table, page_size=page, seq_lens=seq, max_seq_len=60 * page)
+    kv = fb.paged_kv(block_table=table, page_size=page, seq_lens=seq, max_seq_len=400 * page)
     tq, tk, tv = fb.tensor_desc(q[:, None]), fb.mx4_desc(kc, page, D), fb.mx4_desc(vc, page, D)
     need = fb.fl_attn_decode_mx4_workspace_size(tq, tk, kv)
+    assert need > 0
     ws = torch.full((need + 64,), 0x7F, dtype=torch.uint8, device="cuda")
     aux = fb.aux_desc(workspace=ws[:need])
     d = fb.variant_desc(scale=D ** -0.5)

@@ -179,7 +179,8 @@ CALLS = [fb.fl_attn_decode_mx4, fb.fl_attn_prefill_mx4]
     (fb.FL_ERR_SHAPE, dict(q=tensor(2, 1, 3, 3, 64), out=tensor(2, 1, 3, 3, 64))), (fb.FL_ERR_SHAPE, dict(q=tensor(2, 2, 4, 3, 64))), (fb.FL_ERR_SHAPE, dict(vc=pages(n=19))),
     (fb.FL_ERR_SHAPE, dict(kc=pages(page=4), vc=pages(page=4), kv=paged(page=4, max_len=16))), (fb.FL_ERR_SHAPE, dict(kv=paged(stride=2))),
     (fb.FL_ERR_SHAPE, dict(q=tensor(2, 1, 4, 1 << 31, 64))), (fb.FL_ERR_STRIDE, dict(kc=pages(stride={0: 1 << 32}))), (fb.FL_ERR_STRIDE, dict(vc=pages(stride={0: 544}))),
-    (fb.FL_ERR_ALIGN, dict(vc=pages(stride={0: 1096}))), (fb.FL_ERR_ALIGN, dict(kc=pages(ptr=FAKE + 8))), (fb.FL_ERR_ALIGN, dict(a=aux(FAKE + 8))), (fb.FL_ERR_WORKSPACE, dict(a=aux(0))),
+    (fb.FL_ERR_ALIGN, dict(vc=pages(stride={0: 1096}))), (fb.FL_ERR_ALIGN, dict(kc=pages(ptr=FAKE + 8))), (fb.FL_ERR_ALIGN, dict(a=aux(FAKE + 8), kv=paged(max_len=1 << 16, stride=1 << 12))),
+    (fb.FL_ERR_WORKSPACE, dict(a=aux(0), kv=paged(max_len=1 << 16, stride=1 << 12))),
 ])
 def test_attention_refusals(call, want, change):
     a = dict(q=tensor(*T["q"]), kc=pages(), vc=pages(), kv=paged(), d=fb.variant_desc(scale=0.125), a=aux(), out=tensor(*T["q"]), lse=None)
@@ -189,24 +190,28 @@ def test_attention_refusals(call, want, change):
 
 
 def test_attention_workspaces():
-    q, c, kv, d = tensor(*T["q"]), pages(), paged(), fb.variant_desc(scale=0.125)
-    need = fb.fl_attn_decode_mx4_workspace_size(q, c, kv)
-    assert need >= 2 * 3 * 4 * (64 + 2) * 4 and fb.fl_attn_prefill_mx4_workspace_size(q, c, kv) == need
-    for call in CALLS:
-        assert call(q, c, c, kv, d, aux(size=need - 1), q, None) == fb.FL_ERR_WORKSPACE
-    rows = tensor(2, 1, 4, 33, 64)                                              # 66 pairs of a kv head
-    assert fb.fl_attn_decode_mx4(rows, c, c, kv, d, aux(), rows, None) == fb.FL_ERR_SHAPE and "pairs" in fb.fl_last_error_detail()
-    need = fb.fl_attn_prefill_mx4_workspace_size(rows, c, kv)
-    assert need == 2 * 2 * 2 * 64 * 64 * 2
-    assert fb.fl_attn_prefill_mx4(rows, c, c, kv, d, aux(size=need - 1), rows, None) == fb.FL_ERR_WORKSPACE
-    for size in (fb.fl_attn_decode_mx4_workspace_size, fb.fl_attn_prefill_mx4_workspace_size):
-        assert size(None, c, kv) == 0 and size(q, None, kv) == 0 and size(q, c, None) == 0
+    q, c, d = tensor(*T["q"]), pages(), fb.variant_desc(scale=0.125)
+    decode, prefill = fb.fl_attn_decode_mx4_workspace_size, fb.fl_attn_prefill_mx4_workspace_size
+    assert decode(q, c, paged()) == prefill(q, c, paged()) == 0                 # one split: no partial results
     long = paged(max_len=1 << 20, stride=1 << 16)
-    before = fb.fl_attn_decode_mx4_workspace_size(q, c, long)
+    need = decode(q, c, long)
+    assert need == prefill(q, c, long) == 64 * 2 * 3 * 4 * 66 * 4
+    for call in CALLS:
+        assert call(q, c, c, long, d, aux(size=need - 1), q, None) == fb.FL_ERR_WORKSPACE
     assert fb.fl_set_tuning("decode_splits", 3) == fb.FL_OK
-    assert fb.fl_attn_decode_mx4_workspace_size(q, c, long) == 3 * 2 * 3 * 4 * 66 * 4
+    assert decode(q, c, long) == 3 * 2 * 3 * 4 * 66 * 4
     assert fb.fl_set_tuning("decode_splits", 0) == fb.FL_OK
-    assert fb.fl_attn_decode_mx4_workspace_size(q, c, long) == before == 64 * 2 * 3 * 4 * 66 * 4
+    assert decode(q, c, long) == need
+    rows = tensor(2, 1, 4, 33, 64)                                              # 66 pairs of a kv head
+    assert fb.fl_attn_decode_mx4(rows, c, c, paged(), d, aux(), rows, None) == fb.FL_ERR_SHAPE and "pairs" in fb.fl_last_error_detail()
+    # more rows: room for either way, which the call chooses with the mask known
+    assert prefill(rows, c, paged()) == 2 * 2 * 2 * 64 * 64 * 2 and prefill(rows, c, long) >= decode(rows, c, long) > 0
+    many = tensor(64, 1, 4, 4000, 64)
+    need = prefill(many, c, paged(max_len=4096, stride=256))
+    assert need == 2 * 64 * 2 * 4096 * 64 * 2
+    assert fb.fl_attn_prefill_mx4(many, c, c, paged(max_len=4096, stride=256), d, aux(size=need - 1), many, None) == fb.FL_ERR_WORKSPACE
+    for size in (decode, prefill):
+        assert size(None, c, long) == 0 and size(q, None, long) == 0 and size(q, c, None) == 0
 
 
 def test_empty_calls_are_fine():
