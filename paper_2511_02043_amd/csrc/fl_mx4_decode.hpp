@@ -1,4 +1,9 @@
 // Attention over a paged cache in 4 bits for gfx950: the decode step, and the unpacked copy that a long chunk of queries reads.
+//
+// What bounds the step: reading D/2 + D/32 bytes for a key and as many for its value.  Every code has to be converted too, two a lane and instruction, for
+// one query row of a group of heads as for sixteen: 64 sequences of 4k - 8k tokens, 32 / 8 heads, D = 128, take 85 us (5.0 TB/s), with the loads alone 82 - 86,
+// with the arithmetic alone 60 - 65, and 69 at the rate of a large read.  Loads therefore need no registers and no instruction slots beyond their own (rings in LDS, tiles ahead:
+// 104 -> 87 us), and as many waves share a SIMD as the registers allow.
 #pragma once
 #include "fl_decode_bf16.hpp"
 #include "fl_mx4.hpp"
@@ -10,7 +15,8 @@ typedef __attribute__((ext_vector_type(2))) int i32x2;
 
 // Every sequence's cached rows as dense bf16 tensors [B, Hkv, L, D], row j token j, for the forward kernel that a long chunk of queries runs through.
 // Rows from a sequence's length on are left as they are: that kernel is told the length.  A workgroup has 128 keys, or values, of a kv head; a thread has
-// eight channels of every 16th (D = 64: 32nd) of them, all requested before the first is converted, so that a wave stores runs of 1 KB.
+// eight channels of every 16th (D = 64: 32nd) of them, all requested before the first is converted, so that a wave stores runs of 1 KB (8 sequences of 4k - 8k tokens, 8 heads,
+// D = 128: 48 us, 250 MB at the rate of a copy; a row a thread 80).
 constexpr int kUnpackKeys = 128;
 struct Mx4UnpackParams {
   Mx4Cache cache;
@@ -80,7 +86,8 @@ __device__ __forceinline__ float quarter_sum(float x) {
 //     is what the second contraction wants of P: no exchange between lanes;
 //   * for that one, a lane has keys 8 g .. + 7 of channels D/16 m .. + D/16 - 1: the codes of two keys are converted two channels at a time, then
 //     paired key by key.
-// Waves of a SIMD, which are workgroups of a compute unit: what the registers of an instance leave room for.  LDS is shared out among them as rings.
+// Waves of a SIMD, which are workgroups of a compute unit: what the registers of an instance leave room for.  LDS is shared out among them as rings.  (One block: four waves
+// of two stages; three of three are as fast or slower.  Four blocks of 16 pairs would leave one wave: 16 rows of 4 heads 59 us, as two times two blocks 36.)
 constexpr int mx4_decode_waves(int D, int NB) { return NB == 1 ? 4 : 2; }
 template <int D, int NB>
 struct Mx4Ring {

@@ -41,7 +41,8 @@ RowShape shape_row(fl::NormParams* p, int dtype) {
   return r;
 }
 
-// Tokens of a workgroup: enough workgroups for the chip, then enough rows for long runs; their angles take LDS.
+// Tokens of a workgroup: enough workgroups for the chip, then enough rows for long runs; their angles take LDS.  (Forward pass of 2 x 8192 tokens, 32 / 8 heads, us with at
+// least 1024 / 2048 / 4096 / 8192 workgroups: D = 128 70.6 / 68.5 / 67.6 / 72.0, D = 64 33.3 / 32.1 / 32.7 / 39.3, D = 80 44.2 / 44.2 / 46.6 / 54.8.  Appending: below.)
 constexpr int64_t kMostTokens = 16;
 int tokens_of(const fl::NormParams& p, int64_t workgroups) {
   return (int)std::max<int64_t>(1, std::min<int64_t>({(int64_t)p.B * p.S / workgroups, kMostTokens, 16 * 1024 / p.pairs / 8}));
@@ -105,7 +106,8 @@ fl_status view_of(const fl_tensor* t, const char* name, const fl::NormParams& p,
   return st;
 }
 
-// The gradient's launch: enough workgroups for the chip, few enough that their rows of partial sums are soon added up.
+// The gradient's launch: enough workgroups for the chip, few enough that their rows of partial sums are soon added up.  (2 x 8192 tokens, 32 / 8 heads, us with up to 1024 / 2048 /
+// 4096 workgroups, the last with eight heads of a token at most: D = 128 120.5 / 119.0 / 116.8, 32 pairs of it turning 139 / 128 / 140, D = 64 67.5 / 62.9 / 62.9.)
 constexpr int64_t kGradientBlocks = 2048;
 void share_gradient(fl::NormParams* p) {
   p->tokens_per_block = 256 >> p->log_lanes;
