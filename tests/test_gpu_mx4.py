@@ -5,6 +5,8 @@ oracle says where).  Values are codes of what they were: equal bytes.  Attention
 of the sum of their sizes, which stays below 2^6 here: 2.5e-4 in a probability and in the log-sum-exp, with the machine's exponential and logarithm
 2^-11; P enters the second contraction as bf16 (2^-8 of it), the result is rounded to bf16 (2^-8): |error| <= (2^-8 + 2^-10) sum_j P_j |v_j| + 2^-8 |result|.
 """
+import threading
+
 import numpy as np
 import pytest
 import torch
@@ -329,7 +331,7 @@ def test_many_rows_of_long_prompts():
     assert not out[1, :, :7].any() and bool(torch.isneginf(lse[1, :, :7]).all())
 
 
-def test_without_a_table_and_with_other_strides():
+def test_without_a_table_and_with_other_strides(way):
     """A page per sequence of a size that is no power of two; caches that lie head by head."""
     for D in (64, 128):
         B, H, Hkv, size = 3, 4, 2, 72
@@ -356,7 +358,7 @@ def test_without_a_table_and_with_other_strides():
 
 
 @pytest.mark.parametrize("call,rows", [(F.decode_attention_mx4, 2), (F.paged_prefill_attention_mx4, 40)])
-def test_what_lies_behind_a_sequence_is_not_seen(call, rows):
+def test_what_lies_behind_a_sequence_is_not_seen(call, rows, way):
     """Any bytes behind the last token of its last page and in pages behind it: scales of NaN, infinity and zero among them."""
     lens, page, D, Hkv = [77, 40, 129], 16, 128, 2
     kc, vc, table = pool(3, Hkv, D, page, 12)
@@ -374,7 +376,7 @@ def test_what_lies_behind_a_sequence_is_not_seen(call, rows):
         assert same(got[0], want[0]) and same(got[1], want[1]), fill
 
 
-def test_lengths_and_entries_outside_their_bounds_are_cut():
+def test_lengths_and_entries_outside_their_bounds_are_cut(way):
     page, D = 16, 64
     kc, vc, table = pool(3, 2, D, page, 4)
     q = torch.randn(3, 4, D, device="cuda").bfloat16()
@@ -389,7 +391,7 @@ def test_lengths_and_entries_outside_their_bounds_are_cut():
         assert same(call(x, kc, vc, ints([60, 60, 60]), wild), call(x, kc, vc, ints([60, 60, 60]), cut))
 
 
-def test_nothing_cached_at_all():
+def test_nothing_cached_at_all(way):
     kc, vc = F.mx4_cache(4, 16, 2, 64)
     table = torch.zeros(2, 0, dtype=torch.int32, device="cuda")
     for rows, call in ((1, F.decode_attention_mx4), (50, F.paged_prefill_attention_mx4)):
@@ -417,7 +419,7 @@ def test_scores_far_up_and_down():
     assert (np.abs(f64(lse) - ref_lse) <= 5e-3).all()
 
 
-def test_far_pages():
+def test_far_pages(way):
     """Pages more than 2^32 bytes into the caches."""
     page, Hkv, H, D, n = 16, 8, 16, 128, 200
     per, each = -(-n // page), 16 * 68 * 8
@@ -495,7 +497,69 @@ def test_serving_replays_from_a_graph_while_sequences_grow():
         assert same(caches[0][0], caches[1][0]) and same(caches[0][1], caches[1][1])
 
 
-def test_another_stream():
+def test_chunks_replay_from_a_graph_while_sequences_grow(way):
+    """A chunk's append and attention captured together, its sequences longer at every replay; rows split among workgroups and not."""
+    B, H, Hkv, D, page, T = 2, 8, 2, 64, 16, 24
+    for per in (8, 200):
+        caches = [pool(B, Hkv, D, page, per) for _ in range(2)]
+        table = caches[0][2]
+        q, k, v, pos, inv, qw, kw = append_inputs(B, H, Hkv, T, D, (32,))
+        lens = ints([T - 5, T])
+
+        def step(kc, vc):
+            turned = F.norm_rotary_append(q, k, v, pos, inv, kc, vc, lens, table, qw, kw)
+            return (turned,) + F.paged_prefill_attention_mx4(turned, kc, vc, lens, table, return_lse=True)
+
+        side = torch.cuda.Stream()
+        side.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(side):
+            step(*caches[1][:2])
+        torch.cuda.current_stream().wait_stream(side)
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            held = step(*caches[1][:2])
+        for c, old in zip(caches[1][:2], caches[0][:2]):
+            c.copy_(old)
+        for n in range(4):
+            lens += T * (per // 8)
+            pos.add_(T)
+            for x in (q, k, v):
+                x.copy_(torch.randn_like(x))
+            want = step(*caches[0][:2])
+            torch.cuda.synchronize()
+            graph.replay()
+            torch.cuda.synchronize()
+            assert all(same(a, b) for a, b in zip(held, want)), (per, n)
+            assert same(caches[0][0], caches[1][0]) and same(caches[0][1], caches[1][1])
+
+
+def test_calls_of_two_threads():
+    """Each on a stream of its own, several times: what either gives is what it gives alone."""
+    lens, page = [900, 333, 1], 16
+    work = []
+    for D, rows in ((64, 1), (128, 30)):
+        kc, vc, table = pool(3, 2, D, page, 60)
+        q = torch.randn(3, 8, rows, D, device="cuda").bfloat16()
+        call = F.decode_attention_mx4 if rows == 1 else F.paged_prefill_attention_mx4
+        work.append((call, q, kc, vc, ints(lens), table, call(q, kc, vc, ints(lens), table)))
+    torch.cuda.synchronize()
+    wrong = []
+
+    def run(call, q, kc, vc, seq, table, want):
+        with torch.cuda.stream(torch.cuda.Stream()):
+            got = [call(q, kc, vc, seq, table) for _ in range(20)]
+            torch.cuda.current_stream().synchronize()
+        wrong.extend(n for n, g in enumerate(got) if not same(g, want))
+
+    threads = [threading.Thread(target=run, args=w) for w in work]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert not wrong
+
+
+def test_another_stream(way):
     lens, page, D = [3000, 2000], 16, 128
     kc, vc, table = pool(2, 4, D, page, 188)
     q = torch.randn(2, 8, 50, D, device="cuda").bfloat16()
