@@ -66,14 +66,17 @@ __device__ __forceinline__ double group_sum(double x, int lanes) {
   return x;
 }
 
+// STREAM: rows are read past the caches, where a piece of a group of lanes is whole lines of 128 bytes (which a second load would fetch again).  What a norm reads it reads
+// once: 2 x 8192 tokens, 32 / 8 heads, D = 128, forward 68 -> 59 us, gradient 119 -> 100, fp32 66 -> 53 and 117 -> 95 (one of them); with half lines, D = 64, 32 -> 37 and 63 -> 71.
+// (Stores past the caches: 66 and 124.)
 // What a lane has of every row: UPL units of VEC pairs, or of VEC channels that stay (x1 unused then).
-template <class T, int VEC, int UPL, bool INTERLEAVED>
+template <class T, int VEC, int UPL, bool INTERLEAVED, bool STREAM>
 struct NormLane {
   typedef RotaryPiece<T, VEC> Piece;
   typedef RotaryElem<T> E;
+  typedef __attribute__((ext_vector_type(4))) uint32_t Quad;
   int at0[UPL], at1[UPL];
   bool has[UPL], turns[UPL];
-
   int lanes;
 
   __device__ __forceinline__ void init(const NormParams& p, int sub) {
@@ -83,15 +86,26 @@ struct NormLane {
       const int unit = sub + n * lanes, turning = p.pairs / VEC;
       has[n] = unit < p.units;
       turns[n] = unit < turning;
-      at0[n] = turns[n] ? (INTERLEAVED ? 2 * unit * VEC : unit * VEC) : (has[n] ? 2 * p.pairs + (unit - turning) * VEC : 0);
-      at1[n] = turns[n] ? (INTERLEAVED ? at0[n] + VEC : p.pairs + at0[n]) : at0[n];
+      // (VEC neighbouring channels are whole pairs where neighbours pair, so that both kinds have the same pieces; VEC 1: a pair)
+      at0[n] = turns[n] ? (INTERLEAVED && VEC == 1 ? 2 * unit : unit * VEC) : (has[n] ? 2 * p.pairs + (unit - turning) * VEC : 0);
+      at1[n] = turns[n] ? (INTERLEAVED && VEC == 1 ? at0[n] + 1 : p.pairs + at0[n]) : at0[n];
     }
+  }
+  // the number of pair j of unit `unit`
+  __device__ __forceinline__ static int pair_of(const NormParams& p, int unit, int j) {
+    if (!INTERLEAVED || VEC == 1) return unit * VEC + j;
+    return unit * (VEC / 2) + (j < VEC / 2 ? j : p.pairs / 2 + j - VEC / 2);
   }
   __device__ __forceinline__ void load(const T* row, Piece (&x0)[UPL], Piece (&x1)[UPL]) const {
 #pragma unroll
     for (int n = 0; n < UPL; ++n) {                // (lanes without a unit read the row's first channels)
-      x0[n] = *(const Piece*)(row + at0[n]);
-      x1[n] = *(const Piece*)(row + at1[n]);
+      if constexpr (STREAM) {
+        x0[n] = __builtin_bit_cast(Piece, __builtin_nontemporal_load((const Quad*)(row + at0[n])));
+        x1[n] = __builtin_bit_cast(Piece, __builtin_nontemporal_load((const Quad*)(row + at1[n])));
+      } else {
+        x0[n] = *(const Piece*)(row + at0[n]);
+        x1[n] = *(const Piece*)(row + at1[n]);
+      }
     }
   }
   __device__ __forceinline__ void store(T* row, const Piece (&x0)[UPL], const Piece (&x1)[UPL]) const {
@@ -150,12 +164,12 @@ __device__ __forceinline__ int64_t row_at(const View& v, int b, int s) { return 
 
 // Rows [row, row_end) of a workgroup's tokens, `heads` to a token: normalised, weighted and turned from `in` to `out`.  at_in(t), at_out(t): where token t's
 // rows begin (at_out < 0: nowhere).
-template <class T, int VEC, int UPL, bool INTERLEAVED, class In, class Out>
-__device__ __forceinline__ void norm_rows(const NormParams& p, const NormLane<T, VEC, UPL, INTERLEAVED>& l, int sub, const T* in, int64_t in_sh, In at_in, T* out,
+template <class T, int VEC, int UPL, bool INTERLEAVED, bool STREAM, class In, class Out>
+__device__ __forceinline__ void norm_rows(const NormParams& p, const NormLane<T, VEC, UPL, INTERLEAVED, STREAM>& l, int sub, const T* in, int64_t in_sh, In at_in, T* out,
                                           int64_t out_sh, Out at_out, const float* weight, const Divisor& by_heads, int row, int row_end, const float* cs,
                                           const float* sn) {
 #pragma clang fp contract(off)                     // one rounding order in training and in serving
-  typedef NormLane<T, VEC, UPL, INTERLEAVED> L;
+  typedef NormLane<T, VEC, UPL, INTERLEAVED, STREAM> L;
   typedef RotaryElem<T> E;
   constexpr int HU = UPL * VEC <= 8 ? 2 : 1;       // rows whose loads are in flight together
   const int step = 256 >> p.log_lanes;
@@ -197,11 +211,12 @@ __device__ __forceinline__ void norm_rows(const NormParams& p, const NormLane<T,
           z1[j] = E::load(x1[u][n].x[j]) * r * w1[n][j];
         }
         if (l.turns[n]) {
-          const int first = t[u] * p.pairs + (sub + n * l.lanes) * VEC;
+          const int first = t[u] * p.pairs;
 #pragma unroll
           for (int j = 0; j < VEC; ++j) {
             float &a = L::a_of(z0, z1, j), &c = L::b_of(z0, z1, j);
-            const float a_in = a, c_in = c, co = cs[first + j], si = sn[first + j];
+            const int pair = first + L::pair_of(p, sub + n * l.lanes, j);
+            const float a_in = a, c_in = c, co = cs[pair], si = sn[pair];
             a = fmaf(a_in, co, -(c_in * si));
             c = fmaf(c_in, co, a_in * si);
           }
@@ -245,7 +260,7 @@ __device__ __forceinline__ void hold_weights(const NormParams& p, float* w) {
   }
 }
 
-template <class T, int VEC, int UPL, bool INTERLEAVED>
+template <class T, int VEC, int UPL, bool INTERLEAVED, bool STREAM>
 __global__ void __launch_bounds__(256) norm_rotary_kernel(const NormParams p) {
   extern __shared__ int64_t norm_shared[];
   const NormLds x = norm_lds(p, norm_shared, 4);
@@ -263,10 +278,10 @@ __global__ void __launch_bounds__(256) norm_rotary_kernel(const NormParams p) {
   hold_weights(p, x.w);
   form_angles<T>(p, token, n, x.cs, x.sn);
   __syncthreads();
-  NormLane<T, VEC, UPL, INTERLEAVED> l;
+  NormLane<T, VEC, UPL, INTERLEAVED, STREAM> l;
   l.init(p, sub);
   auto rows = [&](const View& in, const View& out, int place, int heads, const Divisor& by, const float* weight) __attribute__((always_inline)) {
-    norm_rows<T, VEC, UPL, INTERLEAVED>(p, l, sub, (const T*)in.ptr, in.sh, [&](int t) { return x.at[4 * t + place]; }, (T*)out.ptr, out.sh,
+    norm_rows<T, VEC, UPL, INTERLEAVED, STREAM>(p, l, sub, (const T*)in.ptr, in.sh, [&](int t) { return x.at[4 * t + place]; }, (T*)out.ptr, out.sh,
                                         [&](int t) { return x.at[4 * t + place + 1]; }, weight, by, 0, n * heads, x.cs, x.sn);
   };
   rows(p.q, p.q_out, 0, p.H, p.by_h, x.w);
@@ -278,9 +293,9 @@ __global__ void __launch_bounds__(256) norm_rotary_kernel(const NormParams p) {
 // D = 64 71 / 63, 512 tokens 18 / 15; here the exchange with LDS and the places of a row cost more than the runs give.)
 // dw gathers in registers, then over the workgroup in LDS, and leaves as a row of partial sums for norm_weights_kernel: no atomics, so that the result does
 // not depend on who comes first.
-template <class T, int VEC, int UPL, bool INTERLEAVED>
+template <class T, int VEC, int UPL, bool INTERLEAVED, bool STREAM>
 __global__ void __launch_bounds__(256) norm_rotary_bwd_kernel(const NormParams p) {
-  typedef NormLane<T, VEC, UPL, INTERLEAVED> L;
+  typedef NormLane<T, VEC, UPL, INTERLEAVED, STREAM> L;
   typedef RotaryElem<T> E;
   extern __shared__ float dw_lds[];                // [waves][D]; before, the weights
   const int sub = threadIdx.x & ((1 << p.log_lanes) - 1), local = threadIdx.x >> p.log_lanes;
@@ -314,7 +329,7 @@ __global__ void __launch_bounds__(256) norm_rotary_bwd_kernel(const NormParams p
       for (int j = 0; j < VEC; ++j) {
         cs[n][j] = 1.f;
         sn[n][j] = 0.f;
-        if (l.turns[n]) E::sincos_turns((float)turn_of(p, (int)token, (sub + n * l.lanes) * VEC + j), sn[n][j], cs[n][j]);
+        if (l.turns[n]) E::sincos_turns((float)turn_of(p, (int)token, L::pair_of(p, sub + n * l.lanes, j)), sn[n][j], cs[n][j]);
       }
     for (int h = h_begin; h < h_end; ++h) {
       float sum[2] = {};                           // of x^2 and of x g
@@ -415,10 +430,10 @@ __global__ void __launch_bounds__(1024) norm_weights_kernel(const NormParams p) 
 // keys', queries' and values' rows, in this order, a part.  A key that is held in 4 bits is computed in 64: its codes are those of the formula's
 // result, and do not depend on the kernel that wrote them.  ALIGNED: a lane's pieces and its neighbours' make whole blocks of 32 channels (VEC = 8,
 // pairs a multiple of 32), so that a key goes from registers to the page; else it is put together in LDS.
-template <int VEC, int UPL, bool INTERLEAVED, bool MX4, bool ALIGNED>
+template <int VEC, int UPL, bool INTERLEAVED, bool STREAM, bool MX4, bool ALIGNED>
 __global__ void __launch_bounds__(256) norm_append_kernel(const NormParams p) {
   typedef uint16_t T;
-  typedef NormLane<T, VEC, UPL, INTERLEAVED> L;
+  typedef NormLane<T, VEC, UPL, INTERLEAVED, STREAM> L;
   typedef RotaryElem<T> E;
   static_assert(!ALIGNED || (MX4 && VEC == 8 && UPL == 1), "pieces of eight channels");
   extern __shared__ int64_t norm_shared[];
@@ -503,7 +518,7 @@ __global__ void __launch_bounds__(256) norm_append_kernel(const NormParams p) {
   };
 
   if constexpr (!MX4) {
-    norm_rows<T, VEC, UPL, INTERLEAVED>(p, l, sub, (const T*)p.k.ptr, p.k.sh, place(2), p.k_cache, p.kc_sh, place(4), x.w + D, p.by_hkv, k_lo, k_hi, x.cs, x.sn);
+    norm_rows<T, VEC, UPL, INTERLEAVED, STREAM>(p, l, sub, (const T*)p.k.ptr, p.k.sh, place(2), p.k_cache, p.kc_sh, place(4), x.w + D, p.by_hkv, k_lo, k_hi, x.cs, x.sn);
   } else if (k_lo < k_hi) {
     float w0[UPL][VEC], w1[UPL][VEC];
     l.weights(x.w + D, w0, w1);
@@ -537,11 +552,12 @@ __global__ void __launch_bounds__(256) norm_append_kernel(const NormParams p) {
           z1[n][j] *= rn * w1[n][j];
         }
         if (l.turns[n]) {
-          const int first = t_now * p.pairs + (sub + n * l.lanes) * VEC;
+          const int first = t_now * p.pairs;
 #pragma unroll
           for (int j = 0; j < VEC; ++j) {
             double &a = L::a_of(z0[n], z1[n], j), &c = L::b_of(z0[n], z1[n], j);
-            const double a_in = a, c_in = c, co = cs64[first + j], si = sn64[first + j];
+            const int pair = first + L::pair_of(p, sub + n * l.lanes, j);
+            const double a_in = a, c_in = c, co = cs64[pair], si = sn64[pair];
             a = a_in * co - c_in * si;
             c = c_in * co + a_in * si;
           }
@@ -550,13 +566,8 @@ __global__ void __launch_bounds__(256) norm_append_kernel(const NormParams p) {
       uint8_t* base = p.mx4.k + h_now * p.mx4.k_sh;
       if constexpr (ALIGNED) {
         int e0 = mx4_own_scale(z0[0]), e1 = mx4_own_scale(z1[0]);
-        if (INTERLEAVED) {                         // turning: 16 channels a lane, in two pieces; staying: eight
-          const int both = max(e0, e1), two = pair_max(both), four = four_max(e0);
-          e0 = e1 = l.turns[0] ? two : four;
-        } else {
-          e0 = four_max(e0);
-          e1 = four_max(e1);
-        }
+        e0 = four_max(e0);
+        e1 = four_max(e1);
         if (real && l.has[0]) put(mx4_pack8(z0[0], e0), e0, l.at0[0], t_now, base, 0, p.k_held, h_now);
         if (real && l.turns[0]) put(mx4_pack8(z1[0], e1), e1, l.at1[0], t_now, base, 0, p.k_held, h_now);
       } else {
@@ -577,7 +588,7 @@ __global__ void __launch_bounds__(256) norm_append_kernel(const NormParams p) {
     }
   }
 
-  norm_rows<T, VEC, UPL, INTERLEAVED>(p, l, sub, (const T*)p.q.ptr, p.q.sh, place(0), (T*)p.q_out.ptr, p.q_out.sh, place(1), x.w, p.by_h, q_lo, q_hi, x.cs,
+  norm_rows<T, VEC, UPL, INTERLEAVED, STREAM>(p, l, sub, (const T*)p.q.ptr, p.q.sh, place(0), (T*)p.q_out.ptr, p.q_out.sh, place(1), x.w, p.by_h, q_lo, q_hi, x.cs,
                                       x.sn);
 
   if constexpr (MX4) {
