@@ -23,7 +23,7 @@ fl_status check_norm(const fl_head_norm* n, fl::NormParams* p) {
 
 // How the kernels share out a row: VEC channels a piece, UPL units a lane.
 struct RowShape {
-  bool wide, streams;
+  bool wide;
   int upl;
 };
 RowShape shape_row(fl::NormParams* p, int dtype) {
@@ -35,8 +35,6 @@ RowShape shape_row(fl::NormParams* p, int dtype) {
   r.upl = r.wide ? (p->units <= 64 ? 1 : 4) : (p->units <= 128 ? 2 : 16);
   p->log_lanes = 0;
   while ((r.upl << p->log_lanes) < p->units) ++p->log_lanes;
-  const int64_t size = dtype == FL_BF16 ? 2 : 4;
-  r.streams = r.wide && r.upl == 1 && p->pairs * size % 128 == 0 && (p->D - 2 * p->pairs) * size % 128 == 0;
   p->by_pairs = fl::Divisor::of(p->pairs);
   p->by_h = fl::Divisor::of(p->H);
   p->by_hkv = fl::Divisor::of(p->Hkv);
@@ -50,18 +48,18 @@ int tokens_of(const fl::NormParams& p, int64_t workgroups) {
   return (int)std::max<int64_t>(1, std::min<int64_t>({(int64_t)p.B * p.S / workgroups, kMostTokens, 16 * 1024 / p.pairs / 8}));
 }
 
-template <class T, int VEC, int UPL, bool STREAM = false>
+template <class T, int VEC, int UPL>
 hipError_t launch_forward(const fl::NormParams& p, bool il, dim3 grid, hipStream_t stream) {
   const size_t lds = fl::norm_lds_bytes(p.tokens_per_block, p.pairs, 4, p.D);
-  if (il) hipLaunchKernelGGL((fl::norm_rotary_kernel<T, VEC, UPL, true, STREAM>), grid, dim3(256), lds, stream, p);
-  else hipLaunchKernelGGL((fl::norm_rotary_kernel<T, VEC, UPL, false, STREAM>), grid, dim3(256), lds, stream, p);
+  if (il) hipLaunchKernelGGL((fl::norm_rotary_kernel<T, VEC, UPL, true>), grid, dim3(256), lds, stream, p);
+  else hipLaunchKernelGGL((fl::norm_rotary_kernel<T, VEC, UPL, false>), grid, dim3(256), lds, stream, p);
   return hipGetLastError();
 }
-template <class T, int VEC, int UPL, bool STREAM = false>
+template <class T, int VEC, int UPL>
 hipError_t launch_gradient(const fl::NormParams& p, bool il, dim3 grid, hipStream_t stream) {
   const size_t lds = 4 * p.D * sizeof(float);
-  if (il) hipLaunchKernelGGL((fl::norm_rotary_bwd_kernel<T, VEC, UPL, true, STREAM>), grid, dim3(256), lds, stream, p);
-  else hipLaunchKernelGGL((fl::norm_rotary_bwd_kernel<T, VEC, UPL, false, STREAM>), grid, dim3(256), lds, stream, p);
+  if (il) hipLaunchKernelGGL((fl::norm_rotary_bwd_kernel<T, VEC, UPL, true>), grid, dim3(256), lds, stream, p);
+  else hipLaunchKernelGGL((fl::norm_rotary_bwd_kernel<T, VEC, UPL, false>), grid, dim3(256), lds, stream, p);
   return hipGetLastError();
 }
 template <int VEC, int UPL, bool MX4, bool ALIGNED = false, bool STREAM = false>
@@ -144,10 +142,10 @@ fl_status fl_norm_rotary(const fl_tensor* q, const fl_tensor* k, const fl_rotary
   hipStream_t s = (hipStream_t)stream;
   hipError_t e;
   if (dtype == FL_BF16)
-    e = r.wide ? (r.streams ? launch_forward<uint16_t, 8, 1, true>(p, il, grid, s) : r.upl == 1 ? launch_forward<uint16_t, 8, 1>(p, il, grid, s) : launch_forward<uint16_t, 8, 4>(p, il, grid, s))
+    e = r.wide ? (r.upl == 1 ? launch_forward<uint16_t, 8, 1>(p, il, grid, s) : launch_forward<uint16_t, 8, 4>(p, il, grid, s))
                : (r.upl == 2 ? launch_forward<uint16_t, 1, 2>(p, il, grid, s) : launch_forward<uint16_t, 1, 16>(p, il, grid, s));
   else
-    e = r.wide ? (r.streams ? launch_forward<float, 4, 1, true>(p, il, grid, s) : r.upl == 1 ? launch_forward<float, 4, 1>(p, il, grid, s) : launch_forward<float, 4, 4>(p, il, grid, s))
+    e = r.wide ? (r.upl == 1 ? launch_forward<float, 4, 1>(p, il, grid, s) : launch_forward<float, 4, 4>(p, il, grid, s))
                : (r.upl == 2 ? launch_forward<float, 1, 2>(p, il, grid, s) : launch_forward<float, 1, 16>(p, il, grid, s));
   return e == hipSuccess ? FL_OK : fail(FL_ERR_LAUNCH, "norm launch: %s", hipGetErrorString(e));
 }
@@ -206,10 +204,10 @@ fl_status fl_norm_rotary_bwd(const fl_tensor* q, const fl_tensor* k, const fl_te
     const dim3 grid((unsigned)p.blocks, (unsigned)(p.q_chunks + p.k_chunks));
     const bool il = rotary->interleaved != 0;
     if (dtype == FL_BF16)
-      e = r.wide ? (r.streams ? launch_gradient<uint16_t, 8, 1, true>(p, il, grid, stream) : r.upl == 1 ? launch_gradient<uint16_t, 8, 1>(p, il, grid, stream) : launch_gradient<uint16_t, 8, 4>(p, il, grid, stream))
+      e = r.wide ? (r.upl == 1 ? launch_gradient<uint16_t, 8, 1>(p, il, grid, stream) : launch_gradient<uint16_t, 8, 4>(p, il, grid, stream))
                  : (r.upl == 2 ? launch_gradient<uint16_t, 1, 2>(p, il, grid, stream) : launch_gradient<uint16_t, 1, 16>(p, il, grid, stream));
     else
-      e = r.wide ? (r.streams ? launch_gradient<float, 4, 1, true>(p, il, grid, stream) : r.upl == 1 ? launch_gradient<float, 4, 1>(p, il, grid, stream) : launch_gradient<float, 4, 4>(p, il, grid, stream))
+      e = r.wide ? (r.upl == 1 ? launch_gradient<float, 4, 1>(p, il, grid, stream) : launch_gradient<float, 4, 4>(p, il, grid, stream))
                  : (r.upl == 2 ? launch_gradient<float, 1, 2>(p, il, grid, stream) : launch_gradient<float, 1, 16>(p, il, grid, stream));
     if (e != hipSuccess) return fail(FL_ERR_LAUNCH, "norm gradient launch: %s", hipGetErrorString(e));
   }
@@ -272,17 +270,17 @@ fl_status fl_norm_rotary_append(const fl_tensor* q, const fl_tensor* k, const fl
   p.tokens_per_block = tokens_of(p, 256);
   const int64_t blocks = (B * T + p.tokens_per_block - 1) / p.tokens_per_block, rows = p.tokens_per_block * (H + 2 * Hkv), at_once = 256 >> p.log_lanes;
   // a column of workgroups shares its tokens' rows, down to one for each group of lanes, while that leaves a compute unit three workgroups at most (8 x 512 tokens,
-  // 32 / 8 heads, D = 128, into 4 bits, 16 tokens a column: 512 or 768 workgroups 24.4 us, 1024 27.1, 1536 27.3)
+  // 32 / 8 heads, D = 128, into 4 bits, 16 tokens a column, inputs from memory: 512 workgroups 28.0 us, 768 25.7, 1024 28.8)
   const int64_t parts = std::max<int64_t>(1, std::min<int64_t>((rows + at_once - 1) / at_once, (768 + blocks - 1) / blocks));
   p.rows_per_part = (int)((rows + parts - 1) / parts);
   const dim3 grid((unsigned)blocks, (unsigned)parts);
-  const bool il = rotary->interleaved != 0;
+  const bool il = rotary->interleaved != 0, streams = r.wide && r.upl == 1 && p.pairs % 64 == 0 && (p.D - 2 * p.pairs) % 64 == 0;
   hipStream_t s = (hipStream_t)stream;
   hipError_t e;
   if (mx4)                                         // (D is 64 or 128)
-    e = !r.wide ? launch_append<1, 2, true>(p, il, grid, s) : (r.streams ? launch_append<8, 1, true, true, true>(p, il, grid, s) : p.pairs % 32 == 0 ? launch_append<8, 1, true, true>(p, il, grid, s) : launch_append<8, 1, true>(p, il, grid, s));
+    e = !r.wide ? launch_append<1, 2, true>(p, il, grid, s) : (streams ? launch_append<8, 1, true, true, true>(p, il, grid, s) : p.pairs % 32 == 0 ? launch_append<8, 1, true, true>(p, il, grid, s) : launch_append<8, 1, true>(p, il, grid, s));
   else
-    e = r.wide ? (r.streams ? launch_append<8, 1, false, false, true>(p, il, grid, s) : r.upl == 1 ? launch_append<8, 1, false>(p, il, grid, s) : launch_append<8, 4, false>(p, il, grid, s))
+    e = r.wide ? (streams ? launch_append<8, 1, false, false, true>(p, il, grid, s) : r.upl == 1 ? launch_append<8, 1, false>(p, il, grid, s) : launch_append<8, 4, false>(p, il, grid, s))
                : (r.upl == 2 ? launch_append<1, 2, false>(p, il, grid, s) : launch_append<1, 16, false>(p, il, grid, s));
   return e == hipSuccess ? FL_OK : fail(FL_ERR_LAUNCH, "append launch: %s", hipGetErrorString(e));
 }

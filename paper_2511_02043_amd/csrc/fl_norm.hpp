@@ -8,7 +8,7 @@
 // angles little.  A row therefore lies in the registers of a few lanes: lane `sub` of a group of them has the row's pairs sub VEC .. (two pieces of VEC channels,
 // 16 bytes each, at D = 128 eight lanes), and the sum is three exchanges between neighbours.  Forwards a workgroup has some tokens: it forms their angles
 // once, one (token, pair) a thread, keeps them in LDS, and goes through the rows in the order of memory, heads of a token first, so that its waves read and
-// write long runs (2 x 8192 tokens, 32 / 8 heads, D = 128, bf16: 68 us, 4.9 TB/s, at the rate of a copy in a trace; lane groups that stay with a token and its angles, pieces of
+// write long runs (2 x 8192 tokens, 32 / 8 heads, D = 128, bf16: 68 - 70 us, 4.8 TB/s; lane groups that stay with a token and its angles, pieces of
 // 256 bytes 12 KB apart, 81).
 #pragma once
 #include "fl_mx4.hpp"
@@ -66,11 +66,11 @@ __device__ __forceinline__ double group_sum(double x, int lanes) {
   return x;
 }
 
-// STREAM: rows are read past the caches, where a piece of a group of lanes is whole lines of 128 bytes (which a second load would fetch again).  What a norm reads it reads
-// once: 2 x 8192 tokens, 32 / 8 heads, D = 128, forward 68 -> 59 us, gradient 119 -> 100, fp32 66 -> 53 and 117 -> 95 (one of them); with half lines, D = 64, 32 -> 37 and 63 -> 71.
-// (Stores past the caches: 66 and 124.)
+// STREAM: rows are read past the caches, where a group of lanes' pieces are whole lines of 128 bytes (a line read in halves would come twice).  For rows on their way into a
+// cache, whose results are read next and they never again: 8 x 512 tokens, 32 / 8 heads, D = 128, into 4 bits 26.5 -> 24.7 us.  Forward pass and gradient gain where their results stay in the
+// caches (68 -> 59 us and 119 -> 100, written to the same place again and again) and nothing where they leave them (192 us both, either way), so they do not.
 // What a lane has of every row: UPL units of VEC pairs, or of VEC channels that stay (x1 unused then).
-template <class T, int VEC, int UPL, bool INTERLEAVED, bool STREAM>
+template <class T, int VEC, int UPL, bool INTERLEAVED, bool STREAM = false>
 struct NormLane {
   typedef RotaryPiece<T, VEC> Piece;
   typedef RotaryElem<T> E;
@@ -260,7 +260,7 @@ __device__ __forceinline__ void hold_weights(const NormParams& p, float* w) {
   }
 }
 
-template <class T, int VEC, int UPL, bool INTERLEAVED, bool STREAM>
+template <class T, int VEC, int UPL, bool INTERLEAVED>
 __global__ void __launch_bounds__(256) norm_rotary_kernel(const NormParams p) {
   extern __shared__ int64_t norm_shared[];
   const NormLds x = norm_lds(p, norm_shared, 4);
@@ -278,24 +278,24 @@ __global__ void __launch_bounds__(256) norm_rotary_kernel(const NormParams p) {
   hold_weights(p, x.w);
   form_angles<T>(p, token, n, x.cs, x.sn);
   __syncthreads();
-  NormLane<T, VEC, UPL, INTERLEAVED, STREAM> l;
+  NormLane<T, VEC, UPL, INTERLEAVED> l;
   l.init(p, sub);
   auto rows = [&](const View& in, const View& out, int place, int heads, const Divisor& by, const float* weight) __attribute__((always_inline)) {
-    norm_rows<T, VEC, UPL, INTERLEAVED, STREAM>(p, l, sub, (const T*)in.ptr, in.sh, [&](int t) { return x.at[4 * t + place]; }, (T*)out.ptr, out.sh,
+    norm_rows<T, VEC, UPL, INTERLEAVED, false>(p, l, sub, (const T*)in.ptr, in.sh, [&](int t) { return x.at[4 * t + place]; }, (T*)out.ptr, out.sh,
                                         [&](int t) { return x.at[4 * t + place + 1]; }, weight, by, 0, n * heads, x.cs, x.sn);
   };
   rows(p.q, p.q_out, 0, p.H, p.by_h, x.w);
   rows(p.k, p.k_out, 2, p.Hkv, p.by_hkv, x.w + p.D);
 }
 
-// The gradient: 117 us at those sizes, 4.3 TB/s of three tensors, and 5 for the weights' sums.  Its rows' angles stay in registers: a group of lanes keeps to a token and goes through the chunk of heads that the workgroup has of it, the next
+// The gradient: 115 us at those sizes, 4.4 TB/s of three tensors, and 5 for the weights' sums.  Its rows' angles stay in registers: a group of lanes keeps to a token and goes through the chunk of heads that the workgroup has of it, the next
 // head's rows on their way while one is worked on.  (us with the rows shared out as in the forward pass / so: 2 x 8192 tokens, 32 / 8 heads, D = 128 121 / 118,
 // D = 64 71 / 63, 512 tokens 18 / 15; here the exchange with LDS and the places of a row cost more than the runs give.)
 // dw gathers in registers, then over the workgroup in LDS, and leaves as a row of partial sums for norm_weights_kernel: no atomics, so that the result does
 // not depend on who comes first.
-template <class T, int VEC, int UPL, bool INTERLEAVED, bool STREAM>
+template <class T, int VEC, int UPL, bool INTERLEAVED>
 __global__ void __launch_bounds__(256) norm_rotary_bwd_kernel(const NormParams p) {
-  typedef NormLane<T, VEC, UPL, INTERLEAVED, STREAM> L;
+  typedef NormLane<T, VEC, UPL, INTERLEAVED> L;
   typedef RotaryElem<T> E;
   extern __shared__ float dw_lds[];                // [waves][D]; before, the weights
   const int sub = threadIdx.x & ((1 << p.log_lanes) - 1), local = threadIdx.x >> p.log_lanes;

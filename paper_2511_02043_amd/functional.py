@@ -586,7 +586,8 @@ def norm_rotary(q: torch.Tensor, k: Optional[torch.Tensor], positions: torch.Ten
 
     q [B, H, S, D], k [B, Hkv, S, D] (or None), positions, inv_freq, sections, interleaved and layouts as for rotary(), D up to 1024; q_weight and
     k_weight float32 [D], shared by the heads (None: ones).  Returns the normalised and turned q and k, in their layouts; differentiable (once)
-    in q, k and both weights, not in inv_freq.  The backward pass reads its inputs again: changed in place before it, they raise there."""
+    in q, k and both weights, not in inv_freq.  The backward pass reads its inputs again: changed in place before it, they raise there.
+    Captured in a graph, it needs leaves that no eager result is still held of, as every backward pass does."""
     if not q.is_cuda or q.dtype not in (torch.bfloat16, torch.float32) or q.dim() != 4:
         raise ValueError("norm_rotary() takes a bf16 or float32 CUDA q of shape [B, H, S, D] (there is no CPU or fallback path)")
     if getattr(inv_freq, "requires_grad", False) and _grad_enabled():
