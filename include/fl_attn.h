@@ -489,7 +489,8 @@ fl_status fl_norm_rotary_append(const fl_tensor* q, const fl_tensor* k, const fl
                                 void* stream);
 
 /* fl_attn_decode over a 4-bit cache: the same arguments and results, with k_cache and v_cache FL_MX4.  Keys and values are bf16 numbers once their codes are
- * read (but for scales near 2^-126), and the arithmetic from there on is that of fl_attn_decode. */
+ * read (but for scales near 2^-126), and the arithmetic from there on is that of fl_attn_decode.  A query row that holds NaN has NaN for its result and an lse that says
+ * nothing; the other rows are as they would be. */
 fl_status fl_attn_decode_mx4(const fl_tensor* q, const fl_tensor* k_cache, const fl_tensor* v_cache, const fl_paged_kv* kv, const fl_variant_desc* desc,
                              const fl_aux* aux, fl_tensor* out, fl_tensor* lse, void* stream);
 

@@ -419,6 +419,35 @@ def test_scores_far_up_and_down():
     assert (np.abs(f64(lse) - ref_lse) <= 5e-3).all()
 
 
+@pytest.mark.parametrize("call,rows,H", [(F.decode_attention_mx4, 1, 8), (F.decode_attention_mx4, 7, 4), (F.paged_prefill_attention_mx4, 45, 4)])
+def test_a_query_row_that_is_not_finite_stays_alone(call, rows, H):
+    lens, page, D, Hkv = [300, 64], 16, 128, 2
+    kc, vc, table = pool(2, Hkv, D, page, 20)
+    q = torch.randn(2, H, rows, D, device="cuda").bfloat16()
+    want, want_lse = call(q, kc, vc, ints(lens), table, return_lse=True)
+    bad = q.clone()
+    bad[0, 1, rows // 2, 3], bad[1, 0, 0, 70] = float("nan"), float("inf")
+    got, lse = call(bad, kc, vc, ints(lens), table, return_lse=True)
+    assert bool(got[0, 1, rows // 2].isnan().all())                  # (its lse says nothing: -inf, as fl_attn_decode's)
+    for x in (got, want, lse, want_lse):
+        x[0, 1, rows // 2], x[1, 0, 0] = 0, 0
+    assert same(got, want) and same(lse, want_lse)
+
+
+def test_weights_that_begin_anywhere():
+    """Weights that are aligned to their four bytes alone."""
+    D, page = 128, 16
+    q, k, v, pos, inv, qw, kw = append_inputs(2, 4, 2, 5, D, (64,))
+    odd = [torch.cat([w.new_zeros(1), w])[1:] for w in (qw, kw)]
+    for a, b in zip(F.norm_rotary(q, k, pos, inv, qw, kw), F.norm_rotary(q, k, pos, inv, *odd)):
+        assert same(a, b)
+    held = []
+    for w in ((qw, kw), odd):
+        kc, vc, table = pool(2, 2, D, page, 3)
+        held.append((F.norm_rotary_append(q, k, v, pos, inv, kc, vc, ints([40, 9]), table, *w), kc, vc))
+    assert all(same(a, b) for a, b in zip(*held))
+
+
 def test_far_pages(way):
     """Pages more than 2^32 bytes into the caches."""
     page, Hkv, H, D, n = 16, 8, 16, 128, 200
