@@ -448,12 +448,12 @@ typedef struct {
  *   q  [B, 1, H, S, D],  k  [B, 1, Hkv, S, D]   bf16 or f32, one dtype; D up to 1024; rows as for fl_rotary_embed
  *   rotary   as for fl_rotary_embed, inverse 0
  *   q_out, k_out   of the same sizes and dtype; may be q and k themselves (in place), no other overlap
- * Sums and products in 32 bits, rounded once. */
+ * Sums and products in 32 bits, rounded once: a row's sum of squares has to be a number there (rows up to 2^58 at any D). */
 fl_status fl_norm_rotary(const fl_tensor* q, const fl_tensor* k, const fl_rotary* rotary, const fl_head_norm* norm, fl_tensor* q_out, fl_tensor* k_out,
                          void* stream);
 
 /* Its gradient.  With dz the gradient that arrives, turned back, r = 1 / sqrt(mean(x^2) + eps) and g = w dz:
- *     dx = r g - r^3 mean(x g) x,      dw = sum over tokens and heads of r x dz
+ *     dx = r (g - u mean(u g)),  u = r x,      dw = sum over tokens and heads of u dz
  *   q, k             as given to fl_norm_rotary (their rows' norms are formed again)
  *   dq_out, dk_out   the gradients that arrive, of the shapes and dtype of q and k (NULL with its input)
  *   dq, dk           written, the same; either may be NULL: not computed

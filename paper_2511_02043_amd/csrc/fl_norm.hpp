@@ -3,7 +3,7 @@
 // Every row x of a query or key head (D channels) becomes
 //     y = R(t) z,   z = w r x,   r = (mean_c x_c^2 + eps)^(-1/2),
 // with R the turn of channel pairs by the positions' angles (fl_rotary.hpp).  Its gradient, with dz = R(-t) dy and g = w dz:
-//     dx = r g - r^3 mean_c(x_c g_c) x,     dw = sum over tokens and heads of r x dz.
+//     dx = r (g - u mean_c(u_c g_c)),  u = r x,     dw = sum over tokens and heads of u dz.
 // An element is read once (the gradient: x and dy) and written once, at some twenty operations: memory traffic, if the row's sum costs no second pass and the
 // angles little.  A row therefore lies in the registers of a few lanes: lane `sub` of a group of them has the row's pairs sub VEC .. (two pieces of VEC channels,
 // 16 bytes each, at D = 128 eight lanes), and the sum is three exchanges between neighbours.  Forwards a workgroup has some tokens: it forms their angles
@@ -365,17 +365,18 @@ __global__ void __launch_bounds__(256) norm_rotary_bwd_kernel(const NormParams p
         }
       }
       group_sum(sum, l.lanes);
-      const float r = 1.f / sqrtf(fmaf(sum[0], inv_d, p.eps)), back = r * r * r * (sum[1] * inv_d);
+      // (r^3 is formed nowhere: it is subnormal from rows of 2^42 on and infinite for rows below 2^-43, where everything else here is an ordinary number)
+      const float r = 1.f / sqrtf(fmaf(sum[0], inv_d, p.eps)), mean = r * (sum[1] * inv_d);     // of u g
       typename L::Piece o0[UPL], o1[UPL];
 #pragma unroll
       for (int n = 0; n < UPL; ++n)
 #pragma unroll
         for (int j = 0; j < VEC; ++j) {
-          const float a = a0[n][j], c = a1[n][j];
-          d0[n][j] = fmaf(a * r, z0[n][j], d0[n][j]);
-          d1[n][j] = fmaf(c * r, z1[n][j], d1[n][j]);
-          o0[n].x[j] = E::store(fmaf(r * w0[n][j], z0[n][j], -a * back));
-          o1[n].x[j] = E::store(fmaf(r * w1[n][j], z1[n][j], -c * back));
+          const float a = a0[n][j] * r, c = a1[n][j] * r;
+          d0[n][j] = fmaf(a, z0[n][j], d0[n][j]);
+          d1[n][j] = fmaf(c, z1[n][j], d1[n][j]);
+          o0[n].x[j] = E::store(r * fmaf(w0[n][j], z0[n][j], -a * mean));
+          o1[n].x[j] = E::store(r * fmaf(w1[n][j], z1[n][j], -c * mean));
         }
       if (ov.ptr != nullptr) l.store(out + h * ov.sh, o0, o1);
     }
