@@ -504,9 +504,13 @@ fl_status fl_attn_prefill_mx4(const fl_tensor* q, const fl_tensor* k_cache, cons
                               const fl_aux* aux, fl_tensor* out, fl_tensor* lse, void* stream);
 
 /* Bytes of aux->workspace that fl_attn_prefill_mx4 needs under any mask: fl_attn_decode_mx4_workspace_size where Sq * H / Hkv <= 64, else the larger of
- * that (up to Sq * H / Hkv = 16384) and the dense copies, 2 * B * Hkv * max_seq_len * D * 2 bytes (each rounded up to 256).  A call that goes the way which
- * needs less takes less. */
+ * that (up to Sq * H / Hkv = 16384) and the dense copies, 2 * B * Hkv * max_seq_len * D * 2 bytes (each rounded up to 256). */
 size_t fl_attn_prefill_mx4_workspace_size(const fl_tensor* q, const fl_tensor* k_cache, const fl_paged_kv* kv);
+
+/* The bytes of them that the call with this desc looks at, which are all that it needs: partial results or none where its rows go through the kernels of
+ * fl_attn_decode_mx4 (64 sequences of 64 rows, 32 / 8 heads, D = 128, under a bound of 131072: none, and 34 GB for the dense copies), else the dense copies.
+ * 0 where the call refuses desc. */
+size_t fl_attn_prefill_mx4_workspace_size_for(const fl_tensor* q, const fl_tensor* k_cache, const fl_paged_kv* kv, const fl_variant_desc* desc);
 
 /* A variant compiled at run time from user expressions (opaque; owned by the caller until released). */
 typedef struct fl_custom_variant fl_custom_variant;

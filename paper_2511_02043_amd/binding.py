@@ -147,6 +147,8 @@ def lib() -> C.CDLL:
         L.fl_attn_decode_mx4.argtypes = L.fl_attn_prefill_mx4.argtypes = L.fl_attn_decode.argtypes
         L.fl_attn_decode_mx4_workspace_size.restype = L.fl_attn_prefill_mx4_workspace_size.restype = C.c_size_t
         L.fl_attn_decode_mx4_workspace_size.argtypes = L.fl_attn_prefill_mx4_workspace_size.argtypes = [TP, TP, C.POINTER(fl_paged_kv)]
+        L.fl_attn_prefill_mx4_workspace_size_for.restype = C.c_size_t
+        L.fl_attn_prefill_mx4_workspace_size_for.argtypes = [TP, TP, C.POINTER(fl_paged_kv), C.POINTER(fl_variant_desc)]
         L.fl_compile_variant.restype = C.c_int
         L.fl_compile_variant.argtypes = [C.c_char_p, C.c_char_p, C.c_uint32, C.c_int, C.POINTER(C.c_void_p)]
         L.fl_attn_fwd_custom.restype = C.c_int
@@ -191,7 +193,7 @@ EXPORTS = ["fl_attn_fwd", "fl_attn_fwd_noalloc", "fl_attn_fwd_workspace_size", "
            "fl_rotary_embed", "fl_rotary_append", "fl_attn_decode_weights", "fl_attn_decode_weights_workspace_size", "fl_key_weights",
            "fl_key_weights_workspace_size", "fl_cache_evict", "fl_norm_rotary", "fl_norm_rotary_bwd", "fl_norm_rotary_bwd_workspace_size",
            "fl_norm_rotary_append", "fl_attn_decode_mx4", "fl_attn_decode_mx4_workspace_size", "fl_attn_prefill_mx4",
-           "fl_attn_prefill_mx4_workspace_size", "fl_release_variant", "fl_variant_supported", "fl_strerror",
+           "fl_attn_prefill_mx4_workspace_size", "fl_attn_prefill_mx4_workspace_size_for", "fl_release_variant", "fl_variant_supported", "fl_strerror",
            "fl_last_error_detail", "fl_set_tuning", "fl_version"]
 
 
@@ -466,6 +468,10 @@ def fl_attn_prefill_mx4(q: fl_tensor, k_cache: fl_tensor, v_cache: fl_tensor, kv
 
 def fl_attn_prefill_mx4_workspace_size(q: fl_tensor, k_cache: fl_tensor, kv: fl_paged_kv) -> int:
     return lib().fl_attn_prefill_mx4_workspace_size(_ref(q), _ref(k_cache), _ref(kv))
+
+
+def fl_attn_prefill_mx4_workspace_size_for(q: fl_tensor, k_cache: fl_tensor, kv: fl_paged_kv, desc: fl_variant_desc) -> int:
+    return lib().fl_attn_prefill_mx4_workspace_size_for(_ref(q), _ref(k_cache), _ref(kv), _ref(desc))
 
 
 def fl_compile_variant(score_mod: Optional[str], mask: Optional[str], D: int, base_mask: int = 0):

@@ -213,6 +213,15 @@ size_t fl_attn_prefill_mx4_workspace_size(const fl_tensor* q, const fl_tensor* k
   return pairs <= kMostPairs && tuned_prefill_gather() != 1 ? split : std::max(split, 2 * dense_bytes(q->size[0], k_cache->size[2], q->size[4], kv->max_seq_len));
 }
 
+size_t fl_attn_prefill_mx4_workspace_size_for(const fl_tensor* q, const fl_tensor* k_cache, const fl_paged_kv* kv, const fl_variant_desc* desc) {
+  if (q == nullptr || k_cache == nullptr || kv == nullptr) return 0;
+  const fl_status st = check_desc(desc);
+  clear_detail();
+  const int64_t B = q->size[0], H = q->size[2], T = q->size[3], D = q->size[4], Hkv = k_cache->size[2], L = kv->max_seq_len;
+  if (st != FL_OK || B <= 0 || H <= 0 || T <= 0 || D <= 0 || Hkv <= 0 || L < 0) return 0;      // (refused, or nothing to do)
+  return through_decode(B, H, Hkv, T, D, L, desc) ? decode_bytes(B, T, H, D, splits_of(B, H, Hkv, T, keys_of(desc, L, T))) : 2 * dense_bytes(B, Hkv, D, L);
+}
+
 fl_status fl_attn_prefill_mx4(const fl_tensor* q, const fl_tensor* k_cache, const fl_tensor* v_cache, const fl_paged_kv* kv, const fl_variant_desc* desc,
                               const fl_aux* aux, fl_tensor* out, fl_tensor* lse, void* stream_v) {
   clear_detail();

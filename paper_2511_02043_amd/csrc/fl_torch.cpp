@@ -574,10 +574,11 @@ std::tuple<int, int64_t, Tensor, OptTensor> paged_4bit(bool decode, const Tensor
     tlse = q.dim() == 3 ? desc5(*lse, {0, -1, 1, -1, -1}) : desc5(*lse, {0, -1, 1, 2, -1});
   }
   const fl_paged_kv kv = paged_mx4(page_size, *lens, table, max_seq_len);
-  const size_t room = std::max<size_t>((decode ? fl_attn_decode_mx4_workspace_size : fl_attn_prefill_mx4_workspace_size)(&tq, &tk, &kv), 16);
+  const fl_variant_desc d = variant(scale, mod, softcap, mask, window, 0, 0);
+  // (a chunk's: what this call looks at, which under any mask may be dense copies of every sequence up to the bound)
+  const size_t room = std::max<size_t>(decode ? fl_attn_decode_mx4_workspace_size(&tq, &tk, &kv) : fl_attn_prefill_mx4_workspace_size_for(&tq, &tk, &kv, &d), 16);
   if (workspace.has_value() && workspace->nbytes() < room) return {0, (int64_t)room, out, lse};
   const Tensor ws = workspace.has_value() ? *workspace : bytes(room, q);
-  const fl_variant_desc d = variant(scale, mod, softcap, mask, window, 0, 0);
   const fl_aux a = aux_of(slopes, std::nullopt, std::nullopt, ws);
   const int status = (decode ? fl_attn_decode_mx4 : fl_attn_prefill_mx4)(&tq, &tk, &tv, &kv, &d, &a, &tout, want_lse ? &tlse : nullptr, (void*)stream);
   return {status, (int64_t)room, out, lse};
