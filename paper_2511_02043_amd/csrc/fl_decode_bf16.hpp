@@ -260,7 +260,7 @@ decode_kernel(const DecodeParams p) {
         const int j = jb + 8 * (r >> 2) + (r & 3);
         float a;
         if constexpr (C::MOD == kModSoftcap) {
-          const float e = fast_exp2(s[r] * (2.f * c_scale / p.softcap));
+          const float e = fast_exp2(s[r] * fminf(2.f * c_scale / p.softcap, 0x1p127f));     // (finite: a raw score of 0 stays 0)
           a = fmaf(fast_rcp(e + 1.f), -2.f * p.softcap * kLog2e, p.softcap * kLog2e);
         } else if constexpr (C::MOD == kModAlibi) {
           a = fmaf(s[r], c_scale, -slope2[cb] * (float)(pos[cb] - j));

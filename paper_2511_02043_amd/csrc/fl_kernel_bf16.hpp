@@ -1002,7 +1002,7 @@ fwd_bf16_kernel(const FwdParams call) {
     // (caps beyond these bounds leave every score 0 in fp32, as the bounds do; in between 1 / (2 cap) is a normal number)
     const float cap = fminf(fmaxf(p.softcap, 0x1p-120f), 0x1p120f);
     auto uniform = [](float x) { return __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(x))); };
-    w.cap_in = uniform(2.f * w.c_scale / cap);
+    w.cap_in = uniform(fminf(2.f * w.c_scale / cap, 0x1p127f));    // (finite: a raw score of 0 stays 0, and there every other one is at the cap)
     w.cap_rcp = uniform(-0.5f / (cap * kLog2e));
     w.cap_l2 = W::kShifted ? -fast_rcp(2.f * w.cap_rcp) : cap * kLog2e;   // (shifted: less this, a raw score of 0 is 0)
   }

@@ -115,7 +115,7 @@ __global__ void __launch_bounds__(C::NW * 64) __attribute__((amdgpu_waves_per_eu
     auto uniform = [](float x) { return __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(x))); };
     const float cap = fminf(fmaxf(p.softcap, 0x1p-120f), 0x1p120f), z1 = p.scale / cap, square = z1 * z1;   // z of a raw score of 1
     cap_l2 = uniform(cap * kLog2e);
-    far_in = uniform(2.f * c_scale / cap);
+    far_in = uniform(fminf(2.f * c_scale / cap, 0x1p127f));
     near0 = uniform(c_scale);
     near1 = uniform(c_scale * kCap1 * square);
     near2 = uniform(c_scale * kCap2 * square * square);

@@ -255,7 +255,7 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(mx4_de
       for (int i = 0; i < 8; ++i) {
         const float raw = s[nb][i >> 2][i & 3];
         if constexpr (MOD == kModSoftcap) {
-          const float e = fast_exp2(raw * (2.f * c_scale / p.softcap));
+          const float e = fast_exp2(raw * fminf(2.f * c_scale / p.softcap, 0x1p127f));     // (finite: a raw score of 0 stays 0)
           x[i] = fmaf(fast_rcp(e + 1.f), -2.f * p.softcap * kLog2e, p.softcap * kLog2e);
         } else if constexpr (MOD == kModAlibi) {
           x[i] = fmaf(raw, c_scale, -slope2[nb] * (float)(pos[nb] - jb - i));
