@@ -29,7 +29,8 @@ int64_t keys_of(const fl_variant_desc* desc, int64_t max_seq_len, int64_t rows) 
 // brings the workgroups to 448 or more, or fewer where a shorter chain of tiles (0.65 us each, of 32 pairs 0.9) does not pay for the merge (3 us, and 1.6 ns and 0.3 a split
 // for each row).  us, 32 / 8 heads, D = 128, splits: 64 sequences of 4k - 8k tokens 1: 87.7, 2: 89.9; 24 of them 1: 45.9, 2: 38.0, 4: 35.7, 8: 38; 8 of them 1: 43,
 // 4: 17.8, 8: 16.9, 16: 18.0; 2 of 100k - 131k 16: 51.9, 32: 52.4, 64: 55.4; 48 of 512 - 1024 1: 12.5, 2: 15.2; eight rows of 24 of 1k - 2k 1: 20.0, 2: 23.8, 3: 28.3.
-// Never more for fewer keys: a workspace that was sized without the window is large enough.
+// Never more for fewer keys: a workspace that was sized without the window is large enough.  (A tile of D = 64 has half the bytes and conversions; its time was not taken apart,
+// and D = 64 goes by the same rule.)
 int splits_of(int64_t B, int64_t H, int64_t Hkv, int64_t T, int64_t keys) {
   const int64_t tiles = (keys + 31) / 32, pairs = pairs_of(H, Hkv, T), units = std::max<int64_t>(1, B * Hkv * blocks_of(pairs));
   if (tuned_decode_splits() > 0) return (int)std::max<int64_t>(1, std::min<int64_t>(tuned_decode_splits(), tiles));

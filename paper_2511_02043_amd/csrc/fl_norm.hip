@@ -270,7 +270,7 @@ fl_status fl_norm_rotary_append(const fl_tensor* q, const fl_tensor* k, const fl
   p.tokens_per_block = tokens_of(p, 256);
   const int64_t blocks = (B * T + p.tokens_per_block - 1) / p.tokens_per_block, rows = p.tokens_per_block * (H + 2 * Hkv), at_once = 256 >> p.log_lanes;
   // a column of workgroups shares its tokens' rows, down to one for each group of lanes, while that leaves a compute unit three workgroups at most (8 x 512 tokens,
-  // 32 / 8 heads, D = 128, into 4 bits, 16 tokens a column, inputs from memory: 512 workgroups 28.0 us, 768 25.7, 1024 28.8)
+  // 32 / 8 heads, D = 128, 16 tokens a column, inputs from memory, with 512 / 768 / 1024 workgroups: into 4 bits 28.7 / 26.2 / 28.8 us, into bf16 pages 23.6 / 22.9 / 23.0)
   const int64_t parts = std::max<int64_t>(1, std::min<int64_t>((rows + at_once - 1) / at_once, (768 + blocks - 1) / blocks));
   p.rows_per_part = (int)((rows + parts - 1) / parts);
   const dim3 grid((unsigned)blocks, (unsigned)parts);

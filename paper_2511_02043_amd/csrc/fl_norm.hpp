@@ -8,7 +8,7 @@
 // angles little.  A row therefore lies in the registers of a few lanes: lane `sub` of a group of them has the row's pairs sub VEC .. (two pieces of VEC channels,
 // 16 bytes each, at D = 128 eight lanes), and the sum is three exchanges between neighbours.  Forwards a workgroup has some tokens: it forms their angles
 // once, one (token, pair) a thread, keeps them in LDS, and goes through the rows in the order of memory, heads of a token first, so that its waves read and
-// write long runs (2 x 8192 tokens, 32 / 8 heads, D = 128, bf16: 68 - 70 us, 4.8 TB/s; lane groups that stay with a token and its angles, pieces of
+// write long runs (2 x 8192 tokens, 32 / 8 heads, D = 128, bf16: 63 - 70 us, 4.8 - 5.3 TB/s; fp32 130; lane groups that stay with a token and its angles, pieces of
 // 256 bytes 12 KB apart, 81).
 #pragma once
 #include "fl_mx4.hpp"
@@ -68,7 +68,8 @@ __device__ __forceinline__ double group_sum(double x, int lanes) {
 
 // STREAM: rows are read past the caches, where a group of lanes' pieces are whole lines of 128 bytes (a line read in halves would come twice).  For rows on their way into a
 // cache, whose results are read next and they never again: 8 x 512 tokens, 32 / 8 heads, D = 128, into 4 bits 26.5 -> 24.7 us.  Forward pass and gradient gain where their results stay in the
-// caches (68 -> 59 us and 119 -> 100, written to the same place again and again) and nothing where they leave them (192 us both, either way), so they do not.
+// caches (68 -> 59 us and 119 -> 100, written to the same place again and again) and lose where they leave them, as in a training step of both (2 x 8192 tokens: 186 us
+// without, 194 with, for the gradient finds part of what the forward pass has read), so they do not.
 // What a lane has of every row: UPL units of VEC pairs, or of VEC channels that stay (x1 unused then).
 template <class T, int VEC, int UPL, bool INTERLEAVED, bool STREAM = false>
 struct NormLane {
@@ -288,7 +289,7 @@ __global__ void __launch_bounds__(256) norm_rotary_kernel(const NormParams p) {
   rows(p.k, p.k_out, 2, p.Hkv, p.by_hkv, x.w + p.D);
 }
 
-// The gradient: 115 us at those sizes, 4.4 TB/s of three tensors, and 5 for the weights' sums.  Its rows' angles stay in registers: a group of lanes keeps to a token and goes through the chunk of heads that the workgroup has of it, the next
+// The gradient: 115 - 118 us at those sizes, 4.3 - 4.4 TB/s of three tensors, and 5 for the weights' sums (fp32 225 and 7).  Its rows' angles stay in registers: a group of lanes keeps to a token and goes through the chunk of heads that the workgroup has of it, the next
 // head's rows on their way while one is worked on.  (us with the rows shared out as in the forward pass / so: 2 x 8192 tokens, 32 / 8 heads, D = 128 121 / 118,
 // D = 64 71 / 63, 512 tokens 18 / 15; here the exchange with LDS and the places of a row cost more than the runs give.)
 // dw gathers in registers, then over the workgroup in LDS, and leaves as a row of partial sums for norm_weights_kernel: no atomics, so that the result does

@@ -299,8 +299,8 @@ def decode_attention(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tens
     stride, e.g. a permuted [pages, Hkv, page_size, D] buffer); seq_lens int32 [B] on the device;
     block_table int32 [B, max_pages] or None for a contiguous cache (sequence b in "page" b).
     max_seq_len is a host-side bound on seq_lens (it fixes the launch shape; default: the capacity
-    of the table, so no device value is read back).  workspace: a uint8 tensor of at least
-    decode_workspace_size(...) bytes to reuse across steps; allocated here when omitted.
+    of the table, so no device value is read back).  workspace: a uint8 tensor to reuse across steps, of at least
+    the bytes that binding.fl_attn_decode_workspace_size() says (a smaller one raises an error that names them); allocated here when omitted.
     Returns out [B, H, D] bf16 (and lse [B, H] float32 with return_lse).  Not differentiable.
     """
     if not q.is_cuda or q.dtype != torch.bfloat16 or q.dim() != 3:
@@ -585,7 +585,7 @@ def norm_rotary(q: torch.Tensor, k: Optional[torch.Tensor], positions: torch.Ten
     weight * x / sqrt(mean(x^2) + eps), whose channel pairs turn as in rotary().
 
     q [B, H, S, D], k [B, Hkv, S, D] (or None), positions, inv_freq, sections, interleaved and layouts as for rotary(), D up to 1024; q_weight and
-    k_weight float32 [D], shared by the heads (None: ones).  Returns the normalised and turned q and k, in their layouts; differentiable (once)
+    k_weight float32 [D], shared by the heads (None: ones).  A row's sum of squares has to be an fp32 number.  Returns the normalised and turned q and k, in their layouts; differentiable (once)
     in q, k and both weights, not in inv_freq.  The backward pass reads its inputs again: changed in place before it, they raise there.
     Captured in a graph, it needs leaves that no eager result is still held of, as every backward pass does."""
     if not q.is_cuda or q.dtype not in (torch.bfloat16, torch.float32) or q.dim() != 4:
@@ -614,7 +614,8 @@ def mx4_cache(pages: int, page_size: int, kv_heads: int, head_dim: int, *, devic
     head_dim 64 or 128; page_size a power of two >= 8 (any multiple of 8 without a block table).  For each page and kv head the
     codes [page_size, head_dim / 2] (channel 2 i in the low half of byte i, 2 i + 1 in the high half; a sign and one of 0, 0.5, 1, 1.5, 2, 3, 4, 6), then the
     scale bytes [head_dim / 32, page_size]: E stands for 2^(E - 127) and belongs to 32 channels of a token.  68 bytes a token and head of 128
-    channels, of 256 in bf16."""
+    channels, of 256 in bf16.  norm_rotary_append(), decode_attention_mx4() and paged_prefill_attention_mx4() take such caches; the calls of a bounded
+    cache (decode_attention_weights(), prefill_key_weights(), evict_cache()) take bf16 pages only."""
     if head_dim not in (64, 128):
         raise ValueError(f"a cache in 4 bits takes heads of 64 or 128 channels, got {head_dim}")
     if page_size < 8 or page_size % 8 != 0:
@@ -631,7 +632,7 @@ def norm_rotary_append(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, positi
     turned keys and the values enter the paged cache at slots seq_lens - T .. seq_lens - 1.
 
     q [B, H, T, D] with k, v [B, Hkv, T, D], or without the T axis for one token; bf16.  q_weight, k_weight float32 [D] or None; eps None: no norms,
-    turns alone.  Caches: bf16 as for rotary_append(), or the two of mx4_cache(), which hold each value in 4 bits with a scale for 32 channels
+    turns alone (into bf16 pages that is rotary_append(), the call for it, which takes heads of any size; the two agree within a rounding).  Caches: bf16 as for rotary_append(), or the two of mx4_cache(), which hold each value in 4 bits with a scale for 32 channels
     (a key is rounded from its exact value; infinities are held as the largest finite value, NaN as zero).  positions, seq_lens,
     block_table, max_seq_len and what is passed over as for rotary_append().  return_held (4-bit caches): also k and v [B, Hkv, (T,) D] bf16 as the
     cache holds them, e.g. for attention() among the rows of a prompt that nothing is cached before.  Not differentiable."""
@@ -665,7 +666,7 @@ def decode_attention_mx4(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.
     """decode_attention() over the two caches of mx4_cache() (fl_attn_decode_mx4): the newest rows of every sequence against its cached keys.
 
     q [B, H, D] (the newest token) or [B, H, T, D] (the newest T, T * H / Hkv <= 64), bf16, D 64 or 128.  Lengths, block_table, max_seq_len,
-    variants, workspace and results as for decode_attention().  Not differentiable."""
+    variants and results as for decode_attention().  workspace: as there, of binding.fl_attn_decode_mx4_workspace_size() bytes.  Not differentiable."""
     if not q.is_cuda or q.dtype != torch.bfloat16 or q.dim() not in (3, 4):
         raise ValueError("decode_attention_mx4() takes a bf16 CUDA q of shape [B, H, D] or [B, H, T, D]")
     return _mx4_call(True, q, k_cache, v_cache, seq_lens, block_table, max_seq_len, scale, window, softcap, alibi_slopes, workspace, return_lse)
@@ -678,7 +679,9 @@ def paged_prefill_attention_mx4(q: torch.Tensor, k_cache: torch.Tensor, v_cache:
     """paged_prefill_attention() over the two caches of mx4_cache() (fl_attn_prefill_mx4): the last Sq tokens of every sequence, already cached, attend
     causally to its cached keys.
 
-    q [B, H, Sq, D] bf16, D 64 or 128; the rest as for paged_prefill_attention().  Not differentiable."""
+    q [B, H, Sq, D] bf16, D 64 or 128; the rest as for paged_prefill_attention().  workspace: at least binding.fl_attn_prefill_mx4_workspace_size_for()
+    bytes, those that this call's way needs (a smaller one raises an error that names them); for many rows they are dense copies of every sequence up to
+    max_seq_len, for which a bound near the longest sequence keeps them small.  Not differentiable."""
     if not q.is_cuda or q.dtype != torch.bfloat16 or q.dim() != 4:
         raise ValueError("paged_prefill_attention_mx4() takes a bf16 CUDA q of shape [B, H, Sq, D]")
     return _mx4_call(False, q, k_cache, v_cache, seq_lens, block_table, max_seq_len, scale, window, softcap, alibi_slopes, workspace, return_lse)
