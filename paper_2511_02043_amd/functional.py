@@ -300,7 +300,7 @@ def decode_attention(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tens
     block_table int32 [B, max_pages] or None for a contiguous cache (sequence b in "page" b).
     max_seq_len is a host-side bound on seq_lens (it fixes the launch shape; default: the capacity
     of the table, so no device value is read back).  workspace: a uint8 tensor to reuse across steps, of at least
-    the bytes that binding.fl_attn_decode_workspace_size() says (a smaller one raises an error that names them); allocated here when omitted.
+    the bytes that binding.fl_attn_decode_workspace_size() says, 16 at least (a smaller one raises an error that names them); allocated here when omitted.
     Returns out [B, H, D] bf16 (and lse [B, H] float32 with return_lse).  Not differentiable.
     """
     if not q.is_cuda or q.dtype != torch.bfloat16 or q.dim() != 3:
@@ -666,7 +666,7 @@ def decode_attention_mx4(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.
     """decode_attention() over the two caches of mx4_cache() (fl_attn_decode_mx4): the newest rows of every sequence against its cached keys.
 
     q [B, H, D] (the newest token) or [B, H, T, D] (the newest T, T * H / Hkv <= 64), bf16, D 64 or 128.  Lengths, block_table, max_seq_len,
-    variants and results as for decode_attention().  workspace: as there, of binding.fl_attn_decode_mx4_workspace_size() bytes.  Not differentiable."""
+    variants and results as for decode_attention().  workspace: as there, of binding.fl_attn_decode_mx4_workspace_size() bytes, 16 at least.  Not differentiable."""
     if not q.is_cuda or q.dtype != torch.bfloat16 or q.dim() not in (3, 4):
         raise ValueError("decode_attention_mx4() takes a bf16 CUDA q of shape [B, H, D] or [B, H, T, D]")
     return _mx4_call(True, q, k_cache, v_cache, seq_lens, block_table, max_seq_len, scale, window, softcap, alibi_slopes, workspace, return_lse)
@@ -680,7 +680,7 @@ def paged_prefill_attention_mx4(q: torch.Tensor, k_cache: torch.Tensor, v_cache:
     causally to its cached keys.
 
     q [B, H, Sq, D] bf16, D 64 or 128; the rest as for paged_prefill_attention().  workspace: at least binding.fl_attn_prefill_mx4_workspace_size_for()
-    bytes, those that this call's way needs (a smaller one raises an error that names them); for many rows they are dense copies of every sequence up to
+    bytes and 16, those that this call's way needs (a smaller one raises an error that names them); for many rows they are dense copies of every sequence up to
     max_seq_len, for which a bound near the longest sequence keeps them small.  Not differentiable."""
     if not q.is_cuda or q.dtype != torch.bfloat16 or q.dim() != 4:
         raise ValueError("paged_prefill_attention_mx4() takes a bf16 CUDA q of shape [B, H, Sq, D]")
